@@ -507,6 +507,132 @@ vt_status vt_layer_decode_emit(const vt_shard_spec* spec, const vt_layer_weights
                                uint32_t phases, const vt_emit* emit, void* ws, size_t ws_bytes,
                                void* stream);
 
+/* ---- Paged KV cache of a batch of sequences (paper Sec. 2.1, LLM Inference:
+ * the cache of each sequence grows as its tokens are generated) ----
+ * A server that runs its shard for several sequences at once keeps their
+ * keys and values in pages of a pool instead of one vt_kv_view each. A page
+ * holds page_size positions of every KV head; a table lists each sequence's
+ * pages in the order of its positions. The steps of a token or a chunk are
+ * vt_paged_append (rotate, store) and then vt_paged_decode_attn or
+ * vt_paged_chunk_attn, both on the same descriptors.
+ *
+ * Everything that changes from step to step (lengths, table, new tokens per
+ * sequence) is device memory that the kernels read, so one captured graph
+ * serves every step. What they hold is checked there: a page outside the
+ * pool is never touched (its keys are not stored, or count as masked), and the
+ * status word says so. */
+
+/* Number formats of activations and of a paged cache. VT_T_F8E4M3 is the OCP
+ * 8-bit float (4 exponent, 3 mantissa bits, largest 448, no infinities); as a
+ * cache format a stored number stands for itself times its head's scale. */
+enum { VT_T_F16 = 0, VT_T_BF16 = 1, VT_T_F8E4M3 = 2 };
+
+/* Bits of the status word. */
+#define VT_PAGED_BAD_PAGE 1u  /* a page number outside 0..n_pages-1 */
+#define VT_PAGED_BAD_LEN 2u   /* a length past max_pages * page_size */
+
+/* The pool and its sequences. Position p of sequence s and KV head h is at
+ *   k + page * page_stride + h * head_stride + (p % page_size) * slot_stride
+ * (elements; the same for v), page = table[s * ld_table + p / page_size].
+ * Any order of heads and slots within a page is therefore possible, and the
+ * contiguous cache of a vt_kv_view is a paged one too: slot_stride head_dim,
+ * head_stride capacity * head_dim, page_stride page_size * head_dim, the table
+ * 0, 1, 2, .. . k and v are 16-byte aligned and the strides positive multiples
+ * of 16 bytes. page_size is a power of two, 1..32768; with 16 and more the
+ * kernels look pages up once per 16 positions (smaller pages work, slower).
+ * Table entries past a sequence's last position are not read. Sequences may
+ * share pages that none of them writes. table, len, the scales and status need
+ * 4-byte alignment only. */
+typedef struct vt_paged_kv {
+  void* k;
+  void* v;
+  int64_t page_stride;
+  int64_t head_stride;
+  int64_t slot_stride;
+  int32_t n_pages;
+  int32_t page_size;
+  int32_t n_kv_heads;
+  int32_t head_dim;        /* 64 or 128 */
+  int32_t type;            /* VT_T_*: the activations' type, or VT_T_F8E4M3 */
+  const float* k_scale;    /* VT_T_F8E4M3 only: device [n_kv_heads], positive; */
+  const float* v_scale;    /*   NULL: 1 */
+  const int32_t* table;    /* device [n_seqs][ld_table >= max_pages] */
+  int64_t ld_table;
+  int32_t max_pages;
+  const int32_t* len;      /* device [n_seqs]: positions filled, this step's tokens included */
+  int32_t n_seqs;
+  uint32_t* status;        /* device, nullable: VT_PAGED_* bits are or-ed in, never cleared */
+} vt_paged_kv;
+
+/* The activations of a step, n_tok rows of consecutive heads, device, type
+ * VT_T_F16 or VT_T_BF16. Rows q_begin[s] .. q_begin[s+1]-1 are sequence s's new
+ * tokens, at its last positions: row r at len[s] - q_begin[s+1] + r.
+ * q_begin is device, [n_seqs + 1], ascending from 0 to at most n_tok; NULL
+ * stands for one token per sequence (row s is sequence s's; n_tok = n_seqs).
+ * Rows behind the last sequence are padding: nothing is read or written for
+ * them. A sequence of length 0 is an idle slot of the batch. */
+typedef struct vt_paged_io {
+  int32_t type;
+  int32_t n_tok;
+  int32_t n_q_heads;       /* a multiple of n_kv_heads; head j uses KV head j / (n_q_heads / n_kv_heads) */
+  const int32_t* q_begin;
+  const void* q;           /* append in, nullable: [n_tok][ld_q >= n_q_heads * head_dim] */
+  int64_t ld_q;
+  const void* k;           /* append in: [n_tok][ld_k >= n_kv_heads * head_dim] */
+  int64_t ld_k;
+  const void* v;           /* append in: [n_tok][ld_v >= n_kv_heads * head_dim] */
+  int64_t ld_v;
+  void* q_rot;             /* append out (if q is given), attention in; may equal q */
+  int64_t ld_qr;
+  void* out;               /* attention out: [n_tok][ld_out >= n_q_heads * head_dim] */
+  int64_t ld_out;
+  float* lse;              /* attention out, nullable: [n_tok][n_q_heads], 4-byte aligned */
+} vt_paged_io;
+
+/* Append flag: rotate elements i and i + head_dim / 2 together instead of the
+ * adjacent pair (2i, 2i + 1). */
+#define VT_ROPE_HALVES 1u
+
+/* Rotate the new tokens' queries and keys by their positions (pair i by the
+ * angle pos * rope_base^(-2i/head_dim); rope_base 0: no rotation) and store keys
+ * and values in their pages. Rotation is fp32 with angles reduced in double,
+ * rounded once, to the type of q_rot or of the cache (VT_T_F8E4M3: of the
+ * number divided by its head's scale, saturating at +-448; NaN stays NaN).
+ * No other byte of the pool changes. A row at a negative position (an idle
+ * slot) is skipped; one past the table or on a bad page is not stored, and
+ * reported in the status word. Two rows must not fall on one slot. */
+vt_status vt_paged_append(const vt_paged_kv* kv, const vt_paged_io* io, float rope_base,
+                          uint32_t flags, void* stream);
+
+/* Bytes of device workspace that vt_paged_decode_attn and vt_paged_chunk_attn
+ * need for these numbers of tokens, heads and sequences (or fewer, at this
+ * head_dim). It must be zero-filled once before its first use by these two
+ * entry points (it is theirs alone: no other entry point's workspace); they
+ * leave its synchronisation words zero after every call. One workspace must not
+ * be used by two calls that may run at the same time (captured graphs that
+ * share one included). */
+vt_status vt_paged_workspace_size(const vt_paged_kv* kv, const vt_paged_io* io, size_t* bytes);
+
+/* Attention of one new token per sequence (io->q_begin NULL) over the paged
+ * cache: for each query head
+ *   out = sum_p softmax_p(scale * q.k_p) v_p,  lse = log sum_p exp(scale * q.k_p)
+ * over the positions p of its sequence, the last ``window`` of them if window
+ * > 0. scale 0 stands for 1/sqrt(head_dim). Scores, sums and lse are fp32; the
+ * weights enter the product with the values as two numbers of the activations'
+ * type, their rounding and its remainder. A query that sees no key (an idle
+ * slot) gets out 0 and lse -infinity. Values and keys outside the visible
+ * positions, and of bad pages, have no influence whatever they hold. With
+ * ``lse`` the results of caches that hold different positions of one sequence
+ * can be joined. */
+vt_status vt_paged_decode_attn(const vt_paged_kv* kv, const vt_paged_io* io, float scale,
+                               int32_t window, void* ws, size_t ws_bytes, void* stream);
+
+/* The same for a chunk of new tokens per sequence (io->q_begin; NULL as
+ * above): the token at position p attends to positions 0..p, the last
+ * ``window`` of them if window > 0. Chunks of any lengths may be mixed. */
+vt_status vt_paged_chunk_attn(const vt_paged_kv* kv, const vt_paged_io* io, float scale,
+                              int32_t window, void* ws, size_t ws_bytes, void* stream);
+
 /* Static text of a status code. */
 const char* vt_status_string(vt_status s);
 

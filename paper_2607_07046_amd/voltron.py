@@ -28,6 +28,9 @@ VT_COOPERATIVE = 0x200
 
 VT_PREC_FP16, VT_PREC_INT8, VT_PREC_INT4, VT_PREC_PRUNED = 0, 1, 2, 3
 VT_W_INT8, VT_W_INT4 = 1, 2
+VT_T_F16, VT_T_BF16, VT_T_F8E4M3 = 0, 1, 2
+VT_PAGED_BAD_PAGE, VT_PAGED_BAD_LEN = 1, 2
+VT_ROPE_HALVES = 1
 VT_WS_ERROR_WORD = 8192  # byte offset of the workspace's barrier error word
 VT_NOALLOC_SCRATCH_BYTES = 4 << 20  # the scratch array of vt_layer_decode_noalloc
 
@@ -37,7 +40,9 @@ EXPORTS = ("vt_shard_spec_create", "vt_shard_spec_query", "vt_shard_spec_destroy
            "vt_qplan", "vt_partial_encode", "vt_partial_decode_add",
            "vt_status_string", "vt_last_error", "vt_quantize_rows", "vt_layer_decode_q",
            "vt_shard_pack", "vt_kv_copy_heads", "vt_moe_workspace_size", "vt_moe_ffn_decode",
-           "vt_stack_decode", "vt_layer_decode_noalloc", "vt_layer_decode_emit")
+           "vt_stack_decode", "vt_layer_decode_noalloc", "vt_layer_decode_emit",
+           "vt_paged_append", "vt_paged_workspace_size", "vt_paged_decode_attn",
+           "vt_paged_chunk_attn")
 
 
 class VoltronError(RuntimeError):
@@ -115,6 +120,28 @@ class vt_kv_stack(ctypes.Structure):
                 ("head_dim", ctypes.c_int32), ("len", ctypes.c_int32)]
 
 
+class vt_paged_kv(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("page_stride", ctypes.c_int64),
+                ("head_stride", ctypes.c_int64), ("slot_stride", ctypes.c_int64),
+                ("n_pages", ctypes.c_int32), ("page_size", ctypes.c_int32),
+                ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("type", ctypes.c_int32), ("k_scale", ctypes.c_void_p),
+                ("v_scale", ctypes.c_void_p), ("table", ctypes.c_void_p),
+                ("ld_table", ctypes.c_int64), ("max_pages", ctypes.c_int32),
+                ("len", ctypes.c_void_p), ("n_seqs", ctypes.c_int32),
+                ("status", ctypes.c_void_p)]
+
+
+class vt_paged_io(ctypes.Structure):
+    _fields_ = [("type", ctypes.c_int32), ("n_tok", ctypes.c_int32),
+                ("n_q_heads", ctypes.c_int32), ("q_begin", ctypes.c_void_p),
+                ("q", ctypes.c_void_p), ("ld_q", ctypes.c_int64),
+                ("k", ctypes.c_void_p), ("ld_k", ctypes.c_int64),
+                ("v", ctypes.c_void_p), ("ld_v", ctypes.c_int64),
+                ("q_rot", ctypes.c_void_p), ("ld_qr", ctypes.c_int64),
+                ("out", ctypes.c_void_p), ("ld_out", ctypes.c_int64), ("lse", ctypes.c_void_p)]
+
+
 class vt_layer_io(ctypes.Structure):
     _fields_ = [("x", ctypes.c_void_p), ("peer_attn", ctypes.c_void_p),
                 ("peer_ffn", ctypes.c_void_p), ("attn_partial", ctypes.c_void_p),
@@ -175,12 +202,20 @@ def load_library(path=None):
     lib.vt_moe_workspace_size.argtypes = [P, I32, I32, ctypes.POINTER(SZ)]
     lib.vt_moe_ffn_decode.argtypes = [P, ctypes.POINTER(vt_moe_weights), I32, I32,
                                       ctypes.POINTER(vt_layer_io), P, P, P, SZ, P]
+    lib.vt_paged_append.argtypes = [ctypes.POINTER(vt_paged_kv), ctypes.POINTER(vt_paged_io),
+                                    ctypes.c_float, U32, P]
+    lib.vt_paged_workspace_size.argtypes = [ctypes.POINTER(vt_paged_kv),
+                                            ctypes.POINTER(vt_paged_io), ctypes.POINTER(SZ)]
+    lib.vt_paged_decode_attn.argtypes = [ctypes.POINTER(vt_paged_kv), ctypes.POINTER(vt_paged_io),
+                                         ctypes.c_float, I32, P, SZ, P]
+    lib.vt_paged_chunk_attn.argtypes = lib.vt_paged_decode_attn.argtypes
     for name in ("vt_shard_spec_create", "vt_shard_spec_query", "vt_kv_append",
                  "vt_workspace_size", "vt_layer_decode", "vt_layer_prefill_chunk",
                  "vt_qplan", "vt_partial_encode", "vt_partial_decode_add",
                  "vt_quantize_rows", "vt_layer_decode_q", "vt_shard_pack", "vt_kv_copy_heads",
                  "vt_moe_workspace_size", "vt_moe_ffn_decode", "vt_stack_decode",
-                 "vt_layer_decode_noalloc", "vt_layer_decode_emit"):
+                 "vt_layer_decode_noalloc", "vt_layer_decode_emit", "vt_paged_append",
+                 "vt_paged_workspace_size", "vt_paged_decode_attn", "vt_paged_chunk_attn"):
         getattr(lib, name).restype = ctypes.c_int
     lib.vt_status_string.argtypes = [ctypes.c_int]
     lib.vt_status_string.restype = ctypes.c_char_p
@@ -335,3 +370,27 @@ def vt_moe_ffn_decode(spec: ShardSpec, w: vt_moe_weights, n_experts, top_k, io: 
     _check(load_library().vt_moe_ffn_decode(spec.handle, ctypes.byref(w), n_experts, top_k,
                                             ctypes.byref(io), sel_out, prob_out, ws, ws_bytes,
                                             stream))
+
+
+def vt_paged_append(kv: vt_paged_kv, io: vt_paged_io, rope_base, flags=0, stream=None):
+    _check(load_library().vt_paged_append(ctypes.byref(kv), ctypes.byref(io), rope_base, flags,
+                                          stream))
+
+
+def vt_paged_workspace_size(kv: vt_paged_kv, io: vt_paged_io) -> int:
+    n = ctypes.c_size_t(0)
+    _check(load_library().vt_paged_workspace_size(ctypes.byref(kv), ctypes.byref(io),
+                                                  ctypes.byref(n)))
+    return n.value
+
+
+def vt_paged_decode_attn(kv: vt_paged_kv, io: vt_paged_io, scale, window, ws, ws_bytes,
+                         stream=None):
+    _check(load_library().vt_paged_decode_attn(ctypes.byref(kv), ctypes.byref(io), scale, window,
+                                               ws, ws_bytes, stream))
+
+
+def vt_paged_chunk_attn(kv: vt_paged_kv, io: vt_paged_io, scale, window, ws, ws_bytes,
+                        stream=None):
+    _check(load_library().vt_paged_chunk_attn(ctypes.byref(kv), ctypes.byref(io), scale, window,
+                                              ws, ws_bytes, stream))
