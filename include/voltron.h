@@ -605,12 +605,12 @@ vt_status vt_paged_append(const vt_paged_kv* kv, const vt_paged_io* io, float ro
                           uint32_t flags, void* stream);
 
 /* Bytes of device workspace that vt_paged_decode_attn and vt_paged_chunk_attn
- * need for these numbers of tokens, heads and sequences (or fewer, at this
- * head_dim). It must be zero-filled once before its first use by these two
- * entry points (it is theirs alone: no other entry point's workspace); they
- * leave its synchronisation words zero after every call. One workspace must not
- * be used by two calls that may run at the same time (captured graphs that
- * share one included). */
+ * need (65 MiB at head_dim 128; the same for every batch at one head_dim). It
+ * must be zero-filled once before its first use by these two entry points (it
+ * is theirs alone: no other entry point's workspace); they leave its
+ * synchronisation words zero after every call. One workspace must not be used
+ * by two calls that may run at the same time (captured graphs that share one
+ * included). */
 vt_status vt_paged_workspace_size(const vt_paged_kv* kv, const vt_paged_io* io, size_t* bytes);
 
 /* Attention of one new token per sequence (io->q_begin NULL) over the paged
@@ -629,7 +629,10 @@ vt_status vt_paged_decode_attn(const vt_paged_kv* kv, const vt_paged_io* io, flo
 
 /* The same for a chunk of new tokens per sequence (io->q_begin; NULL as
  * above): the token at position p attends to positions 0..p, the last
- * ``window`` of them if window > 0. Chunks of any lengths may be mixed. */
+ * ``window`` of them if window > 0. Chunks of any lengths may be mixed. Where
+ * the batch has more than 16 rows (new tokens x query heads per KV head) per
+ * sequence, the weights enter the product with the values rounded once to the
+ * activations' type. */
 vt_status vt_paged_chunk_attn(const vt_paged_kv* kv, const vt_paged_io* io, float scale,
                               int32_t window, void* ws, size_t ws_bytes, void* stream);
 

@@ -17,7 +17,8 @@ OUT = os.path.join(HERE, "libvoltron.so")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 SOURCES = ["spec.cpp", "decode.hip", "moe.hip", "prefill.hip", "comm.hip", "wquant.hip",
-           "repack.hip", "noalloc.hip", "paged.hip", "paged_attn.hip"]
+           "repack.hip", "noalloc.hip", "paged.hip", "paged_attn.hip",
+           "paged_chunk.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-Wno-unused-command-line-argument"]

@@ -93,8 +93,6 @@ struct AttnArgs {
   const int32_t* q_begin;
   int32_t n_tok, n_q, group, window;
   float scale2;  // softmax scale times log2 e
-  // sequences with rows (new tokens x group) in row_min..row_max are this launch's
-  int32_t row_min, row_max;
   uint32_t* arrived;  // one counter per split unit, zero between calls
   float* part;        // partial results of split units
   int32_t target;     // work items to aim at
@@ -178,11 +176,10 @@ struct Share {
   int32_t tiles, block0, blocks;
   __device__ __forceinline__ Share(const AttnArgs& a, const Seq& q) {
     const int64_t rows = static_cast<int64_t>(q.nt) * a.group;
-    const bool mine = rows >= a.row_min && rows <= a.row_max;
-    tiles = mine ? static_cast<int32_t>((rows + ROWS - 1) / ROWS) : 0;
+    tiles = static_cast<int32_t>((rows + ROWS - 1) / ROWS);
     const int lo = a.window > 0 ? max(0, min(max(q.pos0, 0) - (a.window - 1), q.keys)) : 0;
     block0 = lo / KEYS;
-    blocks = mine ? (q.keys - block0 * KEYS + KEYS - 1) / KEYS : 0;
+    blocks = (q.keys - block0 * KEYS + KEYS - 1) / KEYS;
   }
 };
 
@@ -271,10 +268,11 @@ struct Plan {
 };
 
 // ---- host side, in paged.hip -------------------------------------------------
-constexpr int kTarget = 2048;                 // items aimed at, and the number of counters
-constexpr size_t kSyncBytes = kTarget * 4;    // at the start of the workspace
+constexpr int kTarget = 512;          // work items aimed at; fewer units than that are cut, and have counters
+constexpr size_t kSyncBytes = 8192;   // the counters, at the start of the workspace
+static_assert(kTarget * 4 <= kSyncBytes, "");
 
-// Launches the attention of the sequences whose rows are in a.row_min..a.row_max.
+hipError_t launch_chunk(const AttnArgs& a, int type, bool f8, int head_dim, int tile, hipStream_t s);
 hipError_t launch_rows(const AttnArgs& a, int type, bool f8, int head_dim, hipStream_t s);
 
 }  // namespace pg
