@@ -630,7 +630,7 @@ vt_status vt_paged_decode_attn(const vt_paged_kv* kv, const vt_paged_io* io, flo
 /* The same for a chunk of new tokens per sequence (io->q_begin; NULL as
  * above): the token at position p attends to positions 0..p, the last
  * ``window`` of them if window > 0. Chunks of any lengths may be mixed. Where
- * the batch has more than 16 rows (new tokens x query heads per KV head) per
+ * the batch has more than 24 rows (new tokens x query heads per KV head) per
  * sequence, the weights enter the product with the values rounded once to the
  * activations' type. */
 vt_status vt_paged_chunk_attn(const vt_paged_kv* kv, const vt_paged_io* io, float scale,

@@ -253,13 +253,13 @@ size_t part_bytes(int rows, int head_dim) { return static_cast<size_t>(rows) * (
 // Rows of an attention tile, by the mean rows of a sequence (what else the host could
 // know of a batch is on the device): 16 (attn_rows_kernel), 64 or 128 (attn_chunk_kernel).
 // All take every batch; keys and values pass once per tile and a tile's rows cost the
-// same whether they are there or not. Measured with 16 / 64 / 128: 16 sequences of
-// 26 rows on average over up to 4099 positions 79 / 75 / 90 us; one of 4096 rows 658 / 254 /
-// 219 us; 17 rows over 17 positions 6.8 / 7.9 / 7.6 us.
+// same whether they are there or not. Measured with 16 / 64 / 128: one sequence of 17 rows
+// over 17 positions 5.2 / 6.5 / 6.1 us; 16 sequences of 26 rows on average over up to
+// 4099 positions 58.6 / 54.6 / 77; one of 4096 rows 617 / 239 / 206.
 int tile_rows(const vt_paged_kv& kv, const vt_paged_io& io) {
   if (!io.q_begin) return 16;
   const double rows = static_cast<double>(io.n_tok) * (io.n_q_heads / kv.n_kv_heads) / kv.n_seqs;
-  return rows <= 16 ? 16 : (rows <= 64 ? 64 : 128);
+  return rows <= 24 ? 16 : (rows <= 64 ? 64 : 128);
 }
 
 // Fewer than 2 * kTarget pieces of the largest tile: the same for every batch.
@@ -297,11 +297,11 @@ vt_status attend(const vt_paged_kv* kv, const vt_paged_io* io, float scale, int3
                                 1.4426950408889634);
   a.arrived = static_cast<uint32_t*>(ws);
   a.part = reinterpret_cast<float*>(static_cast<char*>(ws) + pg::kSyncBytes);
-  a.target = pg::kTarget;
-  a.min_blocks = 1;
   const bool f8 = kv->type == VT_T_F8E4M3;
   hipStream_t s = static_cast<hipStream_t>(stream);
   const int tile = tile_rows(*kv, *io);
+  a.target = tile == 128 ? pg::kTarget : pg::kTarget / 2;
+  a.min_blocks = tile == 16 ? 2 : 4;
   hipError_t e = tile == 16 ? pg::launch_rows(a, io->type, f8, kv->head_dim, s)
                             : pg::launch_chunk(a, io->type, f8, kv->head_dim, tile, s);
   return e == hipSuccess ? VT_OK : fail(VT_ERR_HIP, "attention launch: %s", hipGetErrorString(e));

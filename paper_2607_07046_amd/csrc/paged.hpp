@@ -132,10 +132,28 @@ __device__ __forceinline__ Seq sequence(const AttnArgs& a, int s) {
 
 // One work item: a tile of a sequence's rows for one KV head, and a piece of its keys.
 struct Item {
+  Seq q;
   int32_t s, tile, head, piece, pieces;
-  int32_t block0, blocks;  // the tile's key blocks, of which this piece takes a share
-  int32_t unit, slot;      // of a split unit: its counter and its first partial result
+  int32_t block0, blocks;  // the sequence's key blocks
+  int32_t unit, slot;      // of a cut unit: its counter and its first partial result
 };
+constexpr int kItemWords = sizeof(Item) / 4;
+
+// Inclusive sum over the lanes of a wave up to each lane: shifts within rows of 16,
+// then the rows' last lanes broadcast into those behind.
+template <int CTRL, int ROW_MASK = 0xF>
+__device__ __forceinline__ int dpp_i(int v) {
+  return __builtin_amdgcn_update_dpp(0, v, CTRL, ROW_MASK, 0xF, false);
+}
+__device__ __forceinline__ int wave_scan(int v) {
+  v += dpp_i<0x111>(v);        // row_shr:1
+  v += dpp_i<0x112>(v);        // row_shr:2
+  v += dpp_i<0x114>(v);        // row_shr:4
+  v += dpp_i<0x118>(v);        // row_shr:8
+  v += dpp_i<0x142, 0xA>(v);   // row_bcast:15 into rows 1 and 3
+  v += dpp_i<0x143, 0xC>(v);   // row_bcast:31 into rows 2 and 3
+  return v;
+}
 
 // Sums of three counts over the threads before this one (the block's totals in tot).
 template <int NT>
@@ -143,14 +161,10 @@ __device__ __forceinline__ void scan3(int (&v)[3], int (&tot)[3], int* lds) {
   const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
   int own[3];
 #pragma unroll
-  for (int i = 0; i < 3; ++i) own[i] = v[i];
-#pragma unroll
-  for (int o = 1; o < kWave; o <<= 1)
-#pragma unroll
-    for (int i = 0; i < 3; ++i) {
-      const int x = __shfl_up(v[i], o, kWave);
-      if (lane >= o) v[i] += x;
-    }
+  for (int i = 0; i < 3; ++i) {
+    own[i] = v[i];
+    v[i] = wave_scan(v[i]);
+  }
   if (lane == kWave - 1)
 #pragma unroll
     for (int i = 0; i < 3; ++i) lds[wave * 3 + i] = v[i];
@@ -188,32 +202,51 @@ struct Share {
 // tiles and heads), units longer than X = max(min_blocks, N / target) blocks are cut
 // into pieces of about equal size. Fewer than ``target`` units are cut, into fewer than
 // 2 * target pieces in all, whatever the lengths: that sizes counters and partials.
+// Up to NT sequences a thread keeps its own one's length from the only load of it.
 template <int ROWS, int KEYS, int NT>
 struct Plan {
   int32_t per;     // sequences per thread
   int32_t most;    // X
   int32_t base[3]; // items, cut units and pieces of them before this thread's sequences
   int32_t total;   // items in all
+  Seq mine;        // this thread's sequence, if it has one only
 
-  __device__ __forceinline__ int pieces(int blocks) const { return max(1, (blocks + most - 1) / most); }
+  // The pieces of a unit are joined by one workgroup, in time that grows with their number:
+  // for tiles of 16 rows a cap that its LDS sets; for the larger ones, whose partial results
+  // are as large as what a stage loads, as many pieces as a piece has blocks.
+  __device__ __forceinline__ int pieces(int blocks) const {
+    const int cap = ROWS == 16 ? 128 : max(1, static_cast<int>(sqrtf(static_cast<float>(blocks))));
+    return min(cap, max(1, (blocks + most - 1) / most));
+  }
 
-  __device__ void make(const AttnArgs& a, int* lds) {
+  __device__ __forceinline__ Seq seq(const AttnArgs& a, int s) const { return per == 1 ? mine : sequence(a, s); }
+
+  __device__ __forceinline__ void cut(const AttnArgs& a, float n) {
+    // n may be rounded: the factor keeps X from falling below N / target
+    most = max(a.min_blocks, static_cast<int32_t>(ceilf(fminf(n * 1.0001f / static_cast<float>(a.target), 1e9f))));
+  }
+
+  __device__ __forceinline__ void make(const AttnArgs& a, int* lds) {
     per = (a.p.n_seqs + NT - 1) / NT;
+    if (a.p.n_seqs == 1) {  // every thread has it, and nothing is to be summed up
+      mine = sequence(a, 0);
+      const Share<ROWS, KEYS> h(a, mine);
+      cut(a, static_cast<float>(h.tiles) * static_cast<float>(h.blocks) * a.p.n_kv);
+      base[0] = base[1] = base[2] = 0;
+      total = h.tiles * a.p.n_kv * pieces(h.blocks);
+      return;
+    }
     const int s0 = threadIdx.x * per, s1 = min(s0 + per, a.p.n_seqs);
-    // units are counted in floating point: exact up to 2^24, and a cut near enough beyond
+    if (per == 1 && s0 < s1) mine = sequence(a, s0);
     float n = 0.f;
     for (int s = s0; s < s1; ++s) {
-      const Seq q = sequence(a, s);
-      const Share<ROWS, KEYS> h(a, q);
+      const Share<ROWS, KEYS> h(a, seq(a, s));
       n += static_cast<float>(h.tiles) * static_cast<float>(h.blocks) * a.p.n_kv;
     }
-    n = block_sum<NT>(n, reinterpret_cast<float*>(lds));
-    // rounding of n is covered by the factor: X must not fall below N / target
-    most = max(a.min_blocks, static_cast<int32_t>(ceilf(fminf(n * 1.0001f / static_cast<float>(a.target), 1e9f))));
+    cut(a, block_sum<NT>(n, reinterpret_cast<float*>(lds)));
     int v[3] = {0, 0, 0}, tot[3];
     for (int s = s0; s < s1; ++s) {
-      const Seq q = sequence(a, s);
-      const Share<ROWS, KEYS> h(a, q);
+      const Share<ROWS, KEYS> h(a, seq(a, s));
       const int units = h.tiles * a.p.n_kv, pc = pieces(h.blocks);
       v[0] += units * pc;
       v[1] += pc > 1 ? units : 0;
@@ -225,50 +258,89 @@ struct Plan {
     total = tot[0];
   }
 
-  // Item i, found by the thread whose sequences hold it and handed to all through
-  // lds (9 words).
-  __device__ Item find(const AttnArgs& a, int i, int* lds) const {
-    const int s0 = threadIdx.x * per, s1 = min(s0 + per, a.p.n_seqs);
-    int at = base[0], unit = base[1], slot = base[2];
-    __syncthreads();
-    for (int s = s0; s < s1 && at <= i; ++s) {
-      const Seq q = sequence(a, s);
-      const Share<ROWS, KEYS> h(a, q);
-      const int units = h.tiles * a.p.n_kv, pc = pieces(h.blocks), n = units * pc;
-      if (i < at + n) {
-        // heads fastest: with a multiple of 8 of them, one head's items share an XCD;
-        // then pieces, then tiles, those with the most keys first
-        int r = i - at;
-        const int head = r % a.p.n_kv;
-        r /= a.p.n_kv;
-        const int piece = r % pc, tile = h.tiles - 1 - r / pc, u = tile * a.p.n_kv + head;
-        lds[0] = s;
-        lds[1] = tile;
-        lds[2] = head;
-        lds[3] = piece;
-        lds[4] = pc;
-        lds[5] = h.block0;
-        lds[6] = h.blocks;
-        lds[7] = unit + u;
-        lds[8] = slot + u * pc;
-      }
-      at += n;
-      if (pc > 1) {
-        unit += units;
-        slot += n;
-      }
-    }
-    __syncthreads();
+  // Item r of sequence s, whose cut units and their pieces start at unit and slot.
+  __device__ __forceinline__ Item item(const AttnArgs& a, const Seq& q, int s, int r, int unit, int slot) const {
+    const Share<ROWS, KEYS> h(a, q);
+    // heads fastest: with a multiple of 8 of them, one head's items share an XCD; then
+    // pieces, then tiles, those with the most keys first
     Item t;
-    int* o = reinterpret_cast<int*>(&t);
+    t.q = q;
+    t.s = s;
+    t.pieces = pieces(h.blocks);
+    t.head = r % a.p.n_kv;
+    r /= a.p.n_kv;
+    t.piece = r % t.pieces;
+    t.tile = h.tiles - 1 - r / t.pieces;
+    t.block0 = h.block0;
+    t.blocks = h.blocks;
+    const int u = t.tile * a.p.n_kv + t.head;
+    t.unit = unit + u;
+    t.slot = slot + u * t.pieces;
+    return t;
+  }
+
+  // Item i, found by the thread whose sequences hold it and handed to all through
+  // lds (kItemWords words).
+  __device__ __forceinline__ Item find(const AttnArgs& a, int i, int* lds) const {
+    Item t;
+    if (a.p.n_seqs == 1) {
+      t = item(a, mine, 0, i, 0, 0);
+    } else {
+      const int s0 = threadIdx.x * per, s1 = min(s0 + per, a.p.n_seqs);
+      int at = base[0], unit = base[1], slot = base[2];
+      __syncthreads();
+      for (int s = s0; s < s1 && at <= i; ++s) {
+        const Seq q = seq(a, s);
+        const Share<ROWS, KEYS> h(a, q);
+        const int units = h.tiles * a.p.n_kv, pc = pieces(h.blocks), n = units * pc;
+        if (i < at + n) {
+          t = item(a, q, s, i - at, unit, slot);
+          const int* w = reinterpret_cast<const int*>(&t);
 #pragma unroll
-    for (int w = 0; w < 9; ++w) o[w] = __builtin_amdgcn_readfirstlane(lds[w]);
+          for (int k = 0; k < kItemWords; ++k) lds[k] = w[k];
+        }
+        at += n;
+        if (pc > 1) {
+          unit += units;
+          slot += n;
+        }
+      }
+      __syncthreads();
+      int* w = reinterpret_cast<int*>(&t);
+#pragma unroll
+      for (int k = 0; k < kItemWords; ++k) w[k] = lds[k];
+    }
+    int* w = reinterpret_cast<int*>(&t);
+#pragma unroll
+    for (int k = 0; k < kItemWords; ++k) w[k] = __builtin_amdgcn_readfirstlane(w[k]);
     return t;
   }
 };
 
+// Item i; false if there is none.
+template <class PLAN>
+__device__ __forceinline__ bool next_item(const AttnArgs& a, int i, Item& t, int* lds) {
+  PLAN plan;
+  plan.make(a, lds);
+  if (i >= plan.total) return false;
+  t = plan.find(a, i, lds);
+  return true;
+}
+
+// Workgroups that cover a batch's items, one each: a cut into pieces of X or more blocks adds
+// at most N / X <= target to the units. The rest ends at once.
+inline uint32_t grid_of(const AttnArgs& a, int64_t tiles, int keys) {
+  const int64_t units = tiles * a.p.n_kv, blocks = (static_cast<int64_t>(a.p.capacity) + keys - 1) / keys;
+  return static_cast<uint32_t>(blocks <= 1 ? units : (units * blocks < units + a.target ? units * blocks : units + a.target));
+}
+
 // ---- host side, in paged.hip -------------------------------------------------
-constexpr int kTarget = 512;          // work items aimed at; fewer units than that are cut, and have counters
+// Work items aimed at by the largest tiles, two workgroups of which a compute unit holds.
+// The smaller tiles aim at half of that, one per compute unit: their pieces wait for
+// memory, and longer ones have less to start, to end and to join (64 sequences of 2000-4097
+// positions, 8 heads: 157 us with 512, 151 with 256; one of 131071 with 8-bit numbers 62
+// and 56; 512 rows per head over 33280 positions on the largest tiles 791 and 1144).
+constexpr int kTarget = 512;
 constexpr size_t kSyncBytes = 8192;   // the counters, at the start of the workspace
 static_assert(kTarget * 4 <= kSyncBytes, "");
 

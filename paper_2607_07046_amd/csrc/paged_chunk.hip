@@ -94,448 +94,449 @@ __global__ void __launch_bounds__(CTH, NG == 1 ? 2 : 1) attn_chunk_kernel(AttnAr
     for (int s = threadIdx.x; s < a.p.n_seqs; s += CTH)
       if (a.p.len[s] > a.p.capacity) sync_or(a.p.status, VT_PAGED_BAD_LEN);
 
-  P plan;
-  plan.make(a, lds);
-  for (int item = blockIdx.x; item < plan.total; item += gridDim.x) {
-    const Item it = plan.find(a, item, lds);
-    const Seq q = sequence(a, it.s);
-    const int rows = q.nt * a.group;
-    int row[NG], khi[NG], klo[NG];
-    bool there[NG];
-    int full_hi = INT32_MAX, any_hi = INT32_MIN, full_lo = INT32_MIN, any_lo = INT32_MAX;
+  Item it;
+  if (!next_item<P>(a, blockIdx.x, it, lds)) return;
+  const Seq& q = it.q;
+  const int rows = q.nt * a.group;
+  int row[NG], khi[NG], klo[NG];
+  bool there[NG];
+  int full_hi = INT32_MAX, any_hi = INT32_MIN, full_lo = INT32_MIN, any_lo = INT32_MAX;
 #pragma unroll
-    for (int g = 0; g < NG; ++g) {
-      const int r = it.tile * C::ROWS + (wr * NG + g) * 32 + ql;
-      there[g] = r < rows;
-      row[g] = min(r, rows - 1);
-      const int pos = q.pos0 + row[g] / a.group;
-      khi[g] = min(pos + 1, q.keys);
-      klo[g] = a.window > 0 ? max(pos, 0) - (a.window - 1) : 0;
-      full_hi = min(full_hi, khi[g]);
-      any_hi = max(any_hi, khi[g]);
-      full_lo = max(full_lo, klo[g]);
-      any_lo = min(any_lo, klo[g]);
-    }
+  for (int g = 0; g < NG; ++g) {
+    const int r = it.tile * C::ROWS + (wr * NG + g) * 32 + ql;
+    there[g] = r < rows;
+    row[g] = min(r, rows - 1);
+    const int pos = q.pos0 + row[g] / a.group;
+    khi[g] = min(pos + 1, q.keys);
+    klo[g] = a.window > 0 ? max(pos, 0) - (a.window - 1) : 0;
+    full_hi = min(full_hi, khi[g]);
+    any_hi = max(any_hi, khi[g]);
+    full_lo = max(full_lo, klo[g]);
+    any_lo = min(any_lo, klo[g]);
+  }
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      full_hi = min(full_hi, __shfl_xor(full_hi, o, kWave));
-      any_hi = max(any_hi, __shfl_xor(any_hi, o, kWave));
-      full_lo = max(full_lo, __shfl_xor(full_lo, o, kWave));
-      any_lo = min(any_lo, __shfl_xor(any_lo, o, kWave));
-    }
-    full_hi = __builtin_amdgcn_readfirstlane(full_hi);
-    any_hi = __builtin_amdgcn_readfirstlane(any_hi);
-    full_lo = __builtin_amdgcn_readfirstlane(full_lo);
-    any_lo = __builtin_amdgcn_readfirstlane(max(any_lo, 0));
+  for (int o = 1; o < 32; o <<= 1) {
+    full_hi = min(full_hi, __shfl_xor(full_hi, o, kWave));
+    any_hi = max(any_hi, __shfl_xor(any_hi, o, kWave));
+    full_lo = max(full_lo, __shfl_xor(full_lo, o, kWave));
+    any_lo = min(any_lo, __shfl_xor(any_lo, o, kWave));
+  }
+  full_hi = __builtin_amdgcn_readfirstlane(full_hi);
+  any_hi = __builtin_amdgcn_readfirstlane(any_hi);
+  full_lo = __builtin_amdgcn_readfirstlane(full_lo);
+  any_lo = __builtin_amdgcn_readfirstlane(max(any_lo, 0));
 
-    // the tile's own key blocks (its last row sees the most, its first one the earliest),
-    // and this piece of them
-    const int tpos0 = q.pos0 + it.tile * C::ROWS / a.group;
-    const int tpos1 = q.pos0 + (min((it.tile + 1) * C::ROWS, rows) - 1) / a.group;
-    const int thi = max(0, min(tpos1 + 1, q.keys)), tlo = a.window > 0 ? max(0, max(tpos0, 0) - (a.window - 1)) : 0;
-    const int tb0 = tlo / KS, tbn = max(0, (thi + KS - 1) / KS - tb0);
-    const int b0 = tb0 + static_cast<int>(static_cast<int64_t>(tbn) * it.piece / it.pieces);
-    const int stages = tb0 + static_cast<int>(static_cast<int64_t>(tbn) * (it.piece + 1) / it.pieces) - b0;
-    const char* kb = a.p.k + it.head * a.p.head;
-    const char* vb = a.p.v + it.head * a.p.head;
-    const uint32_t slot = static_cast<uint32_t>(a.p.slot);
-    const int last = q.keys - 1;  // no position past it is read or looked up
-    const int32_t* tabv = a.p.table + it.s * a.p.ld_table;
-    ConstInt* tab = constant(tabv);
+  // the tile's own key blocks (its last row sees the most, its first one the earliest),
+  // and this piece of them
+  const int tpos0 = q.pos0 + it.tile * C::ROWS / a.group;
+  const int tpos1 = q.pos0 + (min((it.tile + 1) * C::ROWS, rows) - 1) / a.group;
+  const int thi = max(0, min(tpos1 + 1, q.keys)), tlo = a.window > 0 ? max(0, max(tpos0, 0) - (a.window - 1)) : 0;
+  const int tb0 = tlo / KS, tbn = max(0, (thi + KS - 1) / KS - tb0);
+  const int b0 = tb0 + static_cast<int>(static_cast<int64_t>(tbn) * it.piece / it.pieces);
+  const int stages = tb0 + static_cast<int>(static_cast<int64_t>(tbn) * (it.piece + 1) / it.pieces) - b0;
+  const char* kb = a.p.k + it.head * a.p.head;
+  const char* vb = a.p.v + it.head * a.p.head;
+  const uint32_t slot = static_cast<uint32_t>(a.p.slot);
+  const int last = q.keys - 1;  // no position past it is read or looked up
+  const int32_t* tabv = a.p.table + it.s * a.p.ld_table;
+  ConstInt* tab = constant(tabv);
 
-    u32x4 qf[NG][NK];
+  u32x4 qf[NG][NK];
 #pragma unroll
-    for (int g = 0; g < NG; ++g) {
-      const int tok = row[g] / a.group, j = row[g] - tok * a.group;
-      const uint16_t* qp = a.q + (q.b + tok) * a.ld_q + (static_cast<int64_t>(it.head) * a.group + j) * D;
+  for (int g = 0; g < NG; ++g) {
+    const int tok = row[g] / a.group, j = row[g] - tok * a.group;
+    const uint16_t* qp = a.q + (q.b + tok) * a.ld_q + (static_cast<int64_t>(it.head) * a.group + j) * D;
 #pragma unroll
-      for (int c = 0; c < NK; ++c) qf[g][c] = load16(qp + c * 16 + 8 * hf);
+    for (int c = 0; c < NK; ++c) qf[g][c] = load16(qp + c * 16 + 8 * hf);
+  }
+  const float sc = a.scale2 * (F8 && a.p.k_scale ? a.p.k_scale[it.head] : 1.f);
+
+  f32x16 o[NG][NM];
+  float ref[NG], sum[NG];
+#pragma unroll
+  for (int g = 0; g < NG; ++g) {
+    ref[g] = -INFINITY;
+    sum[g] = 0.f;
+#pragma unroll
+    for (int m = 0; m < NM; ++m) o[g][m] = f32x16{};
+  }
+
+  // ---- stages into LDS -------------------------------------------------------
+  // A stage's page numbers are looked up a stage ahead of its loads. IDS: those a
+  // lane needs, of loads u of its wave.
+  constexpr int LPW = F8 ? D / 64 : D / 32;          // loads of K (and of V) per wave: 16 rows, or (8-bit) 8 or 16 of them
+  constexpr int RPL = F8 ? 1024 / D : 512 / D;       // rows of a load
+  constexpr int LPR = kWave / RPL;                   // lanes of a row
+  const int lrow = lane / LPR, lcol = lane % LPR;
+  // rows of load u of this wave in the stage
+  auto first_row = [&](int u) { return F8 ? u * (CW * RPL) + wave * RPL : wave * 16 + u * RPL; };
+  int ids[BIG ? (F8 ? LPW : 1) : LPW];
+  u32x4 kreg[F8 ? LPW : 1], vreg[F8 ? LPW : 1];
+  auto look = [&](int st) {
+    const int p0 = (b0 + min(st, stages - 1)) * KS;
+    if constexpr (BIG) {
+#pragma unroll
+      for (int u = 0; u < (F8 ? LPW : 1); ++u) ids[u] = tab[min(p0 + first_row(u), last) >> a.p.shift];
+    } else {
+#pragma unroll
+      for (int u = 0; u < LPW; ++u) ids[u] = tabv[min(p0 + first_row(u) + lrow, last) >> a.p.shift];
     }
-    const float sc = a.scale2 * (F8 && a.p.k_scale ? a.p.k_scale[it.head] : 1.f);
-
-    f32x16 o[NG][NM];
-    float ref[NG], sum[NG];
+  };
+  auto fetch = [&](int st) {
+    const int p0 = (b0 + min(st, stages - 1)) * KS;
+    const uint32_t to = lbase + (st % C::NST) * C::STAGE;
+    uint32_t gone = 0;  // bad pages among the rows of the wave's loads so far
 #pragma unroll
-    for (int g = 0; g < NG; ++g) {
-      ref[g] = -INFINITY;
-      sum[g] = 0.f;
-#pragma unroll
-      for (int m = 0; m < NM; ++m) o[g][m] = f32x16{};
-    }
-
-    // ---- stages into LDS -------------------------------------------------------
-    // A stage's page numbers are looked up a stage ahead of its loads. IDS: those a
-    // lane needs, of loads u of its wave.
-    constexpr int LPW = F8 ? D / 64 : D / 32;          // loads of K (and of V) per wave: 16 rows, or (8-bit) 8 or 16 of them
-    constexpr int RPL = F8 ? 1024 / D : 512 / D;       // rows of a load
-    constexpr int LPR = kWave / RPL;                   // lanes of a row
-    const int lrow = lane / LPR, lcol = lane % LPR;
-    // rows of load u of this wave in the stage
-    auto first_row = [&](int u) { return F8 ? u * (CW * RPL) + wave * RPL : wave * 16 + u * RPL; };
-    int ids[BIG ? (F8 ? LPW : 1) : LPW];
-    u32x4 kreg[F8 ? LPW : 1], vreg[F8 ? LPW : 1];
-    auto look = [&](int st) {
-      const int p0 = (b0 + min(st, stages - 1)) * KS;
+    for (int u = 0; u < LPW; ++u) {
+      const int id = ids[BIG ? (F8 ? u : 0) : u];
+      const bool ok = id >= 0 && id < a.p.n_pages;
+      const int64_t page = static_cast<int64_t>(ok ? id : 0) * a.p.page;
       if constexpr (BIG) {
-#pragma unroll
-        for (int u = 0; u < (F8 ? LPW : 1); ++u) ids[u] = tab[min(p0 + first_row(u), last) >> a.p.shift];
+        if (!ok) gone |= ((1u << RPL) - 1) << (F8 ? 0 : u * RPL);
       } else {
+        const uint64_t m = __builtin_amdgcn_ballot_w64(!ok);
+        if (m)
 #pragma unroll
-        for (int u = 0; u < LPW; ++u) ids[u] = tabv[min(p0 + first_row(u) + lrow, last) >> a.p.shift];
+          for (int i = 0; i < RPL; ++i) gone |= static_cast<uint32_t>(m >> (i * LPR) & 1) << (F8 ? i : u * RPL + i);
       }
-    };
-    auto fetch = [&](int st) {
-      const int p0 = (b0 + min(st, stages - 1)) * KS;
-      const uint32_t to = lbase + (st % C::NST) * C::STAGE;
-      uint32_t gone = 0;  // bad pages among the rows of the wave's loads so far
+      if (F8 || u == LPW - 1) {
+        char* flag = reinterpret_cast<char*>(absent[st % C::NST]) + (F8 ? first_row(u) : wave * 16) / 8;
+        if (lane == 0) {
+          if (F8 && RPL == 8) *reinterpret_cast<uint8_t*>(flag) = static_cast<uint8_t>(gone);
+          else *reinterpret_cast<uint16_t*>(flag) = static_cast<uint16_t>(gone);
+        }
+        gone = 0;
+      }
+      const int r0 = first_row(u), r = r0 + lrow;
+      const char *kp, *vp;  // of the lane's row
+      uint32_t off = 0;
+      if constexpr (BIG) {
+        const int key = min(p0 + r0, last);
+        const int64_t at = page + static_cast<int64_t>(key & a.p.mask) * a.p.slot;
+        kp = kb + at;
+        vp = vb + at;
+        off = static_cast<uint32_t>(min(lrow, last - key)) * slot;  // rows past the last position read that one again
+      } else {
+        const int64_t at = page + static_cast<int64_t>(min(p0 + r, last) & a.p.mask) * a.p.slot;
+        kp = kb + at;
+        vp = vb + at;
+      }
+      if constexpr (F8) {
+        kreg[u] = *reinterpret_cast<const u32x4*>(kp + off + lcol * 16);
+        vreg[u] = *reinterpret_cast<const u32x4*>(vp + off + lcol * 16);
+      } else {
+        const uint32_t kc = (lcol ^ (r % CPR)) * 16, vc = (lcol ^ (2 * (r % (CPR / 2)))) * 16;
+        const uint32_t tk = __builtin_amdgcn_readfirstlane(to + r0 * D * 2);
+        if constexpr (BIG) {
+          dma_rows(tk, kp, off + kc);
+          dma_rows(tk + KV, vp, off + vc);
+        } else {
+          dma_lanes(tk, kp + kc);
+          dma_lanes(tk + KV, vp + vc);
+        }
+      }
+    }
+  };
+  // 8-bit: what fetch loaded, widened into its stage
+  auto widen = [&](int st) {
+    if constexpr (F8) {
+      char* S = smem + (st % C::NST) * C::STAGE;
 #pragma unroll
       for (int u = 0; u < LPW; ++u) {
-        const int id = ids[BIG ? (F8 ? u : 0) : u];
-        const bool ok = id >= 0 && id < a.p.n_pages;
-        const int64_t page = static_cast<int64_t>(ok ? id : 0) * a.p.page;
-        if constexpr (BIG) {
-          if (!ok) gone |= ((1u << RPL) - 1) << (F8 ? 0 : u * RPL);
-        } else {
-          const uint64_t m = __builtin_amdgcn_ballot_w64(!ok);
-          if (m)
-#pragma unroll
-            for (int i = 0; i < RPL; ++i) gone |= static_cast<uint32_t>(m >> (i * LPR) & 1) << (F8 ? i : u * RPL + i);
-        }
-        if (F8 || u == LPW - 1) {
-          char* flag = reinterpret_cast<char*>(absent[st % C::NST]) + (F8 ? first_row(u) : wave * 16) / 8;
-          if (lane == 0) {
-            if (F8 && RPL == 8) *reinterpret_cast<uint8_t*>(flag) = static_cast<uint8_t>(gone);
-            else *reinterpret_cast<uint16_t*>(flag) = static_cast<uint16_t>(gone);
-          }
-          gone = 0;
-        }
-        const int r0 = first_row(u), r = r0 + lrow;
-        const char *kp, *vp;  // of the lane's row
-        uint32_t off = 0;
-        if constexpr (BIG) {
-          const int key = min(p0 + r0, last);
-          const int64_t at = page + static_cast<int64_t>(key & a.p.mask) * a.p.slot;
-          kp = kb + at;
-          vp = vb + at;
-          off = static_cast<uint32_t>(min(lrow, last - key)) * slot;  // rows past the last position read that one again
-        } else {
-          const int64_t at = page + static_cast<int64_t>(min(p0 + r, last) & a.p.mask) * a.p.slot;
-          kp = kb + at;
-          vp = vb + at;
-        }
-        if constexpr (F8) {
-          kreg[u] = *reinterpret_cast<const u32x4*>(kp + off + lcol * 16);
-          vreg[u] = *reinterpret_cast<const u32x4*>(vp + off + lcol * 16);
-        } else {
-          const uint32_t kc = (lcol ^ (r % CPR)) * 16, vc = (lcol ^ (2 * (r % (CPR / 2)))) * 16;
-          const uint32_t tk = __builtin_amdgcn_readfirstlane(to + r0 * D * 2);
-          if constexpr (BIG) {
-            dma_rows(tk, kp, off + kc);
-            dma_rows(tk + KV, vp, off + vc);
-          } else {
-            dma_lanes(tk, kp + kc);
-            dma_lanes(tk + KV, vp + vc);
-          }
-        }
-      }
-    };
-    // 8-bit: what fetch loaded, widened into its stage
-    auto widen = [&](int st) {
-      if constexpr (F8) {
-        char* S = smem + (st % C::NST) * C::STAGE;
-#pragma unroll
-        for (int u = 0; u < LPW; ++u) {
-          const int r = first_row(u) + lrow;
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            u32x4 w, x;
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              w[2 * e] = T::template from_f8<false>(kreg[u][2 * h + e]);
-              w[2 * e + 1] = T::template from_f8<true>(kreg[u][2 * h + e]);
-              x[2 * e] = T::template from_f8<false>(vreg[u][2 * h + e]);
-              x[2 * e + 1] = T::template from_f8<true>(vreg[u][2 * h + e]);
-            }
-            const int c = 2 * lcol + h;
-            *reinterpret_cast<u32x4*>(S + r * D * 2 + (c ^ (r % CPR)) * 16) = w;
-            *reinterpret_cast<u32x4*>(S + KV + r * D * 2 + (c ^ (2 * (r % (CPR / 2)))) * 16) = x;
-          }
-        }
-      }
-    };
-
-    // ---- one block of 32 keys ------------------------------------------------------
-    const int grp = lane / 16, jl = lane % 16;
-    const int vkey = 8 * (grp / 2) + jl / 4, vdim = 2 * (grp % 2) + (jl % 4) / 2;
-    const int kr = swap_bits23(ql);
-    // scores to weights, sums and the second product's operand
-    auto weigh = [&](f32x16 (&s)[NG], u32x4 (&pf)[NG][2]) {
-#pragma unroll
-      for (int g = 0; g < NG; ++g) {
-        float top = s[g][0];
-#pragma unroll
-        for (int i = 1; i < 16; ++i) top = fmaxf(top, s[g][i]);
-        top *= sc;
-        if (__builtin_amdgcn_ballot_w64(top > ref[g] + 8.f) != 0) {
-          top = fmaxf(top, __shfl_xor(top, 32, kWave));
-          const float next = fmaxf(top, ref[g]);
-          const float alpha = next == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ref[g] - next);
-          ref[g] = next;
-          sum[g] *= alpha;
-#pragma unroll
-          for (int m = 0; m < NM; ++m)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) o[g][m][i] *= alpha;
-        }
-        const float base = ref[g] == -INFINITY ? 0.f : ref[g];
-#pragma unroll
-        for (int w = 0; w < 8; ++w) {
-          const float pa = __builtin_amdgcn_exp2f(fmaf(s[g][2 * w], sc, -base));
-          const float pb = __builtin_amdgcn_exp2f(fmaf(s[g][2 * w + 1], sc, -base));
-          sum[g] += pa + pb;
-          pf[g][w / 4][w % 4] = T::pack2(pa, pb);
-        }
-      }
-    };
-    // the block at S (K's rows; V's KV bytes behind), from key p0 on; gone: its keys on bad pages
-    auto block = [&](const char* S, int p0, uint32_t gone) {
-      f32x16 s[NG];
-      u32x4 pf[NG][2];
-#pragma unroll
-      for (int g = 0; g < NG; ++g) s[g] = f32x16{};
-#pragma unroll
-      for (int c = 0; c < NK; ++c) {
-        const u32x4 kf = *reinterpret_cast<const u32x4*>(S + (kr * D * 2 + ((2 * c + hf) ^ (kr % CPR)) * 16));
-#pragma unroll
-        for (int g = 0; g < NG; ++g) s[g] = T::mfma32(kf, qf[g][c], s[g]);
-      }
-      auto vfrag = [&](int m, int b) {
-        u32x4 f;
+        const int r = first_row(u) + lrow;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          const int r = vkey + 4 * h;
-          const u32x2 x = lds_read_tr(S + KV + 16 * b * D * 2 +
-                                      (r * D * 2 + ((4 * m + vdim) ^ (2 * (r % (CPR / 2)))) * 16 + (jl % 2) * 8));
-          f[2 * h] = x[0];
-          f[2 * h + 1] = x[1];
+          u32x4 w, x;
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            w[2 * e] = T::template from_f8<false>(kreg[u][2 * h + e]);
+            w[2 * e + 1] = T::template from_f8<true>(kreg[u][2 * h + e]);
+            x[2 * e] = T::template from_f8<false>(vreg[u][2 * h + e]);
+            x[2 * e + 1] = T::template from_f8<true>(vreg[u][2 * h + e]);
+          }
+          const int c = 2 * lcol + h;
+          *reinterpret_cast<u32x4*>(S + r * D * 2 + (c ^ (r % CPR)) * 16) = w;
+          *reinterpret_cast<u32x4*>(S + KV + r * D * 2 + (c ^ (2 * (r % (CPR / 2)))) * 16) = x;
         }
-        return f;
-      };
-      if (p0 >= full_lo && p0 + 32 <= full_hi && gone == 0) {  // all rows of the wave see all of it
-        weigh(s, pf);
+      }
+    }
+  };
+
+  // ---- one block of 32 keys ------------------------------------------------------
+  const int grp = lane / 16, jl = lane % 16;
+  const int vkey = 8 * (grp / 2) + jl / 4, vdim = 2 * (grp % 2) + (jl % 4) / 2;
+  const int kr = swap_bits23(ql);
+  // scores to weights, sums and the second product's operand
+  auto weigh = [&](f32x16 (&s)[NG], u32x4 (&pf)[NG][2]) {
+#pragma unroll
+    for (int g = 0; g < NG; ++g) {
+      float top = s[g][0];
+#pragma unroll
+      for (int i = 1; i < 16; ++i) top = fmaxf(top, s[g][i]);
+      top *= sc;
+      if (__builtin_amdgcn_ballot_w64(top > ref[g] + 8.f) != 0) {
+        top = fmaxf(top, __shfl_xor(top, 32, kWave));
+        const float next = fmaxf(top, ref[g]);
+        const float alpha = next == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ref[g] - next);
+        ref[g] = next;
+        sum[g] *= alpha;
 #pragma unroll
         for (int m = 0; m < NM; ++m)
 #pragma unroll
-          for (int b = 0; b < 2; ++b) {
-            const u32x4 vf = vfrag(m, b);
-#pragma unroll
-            for (int g = 0; g < NG; ++g) o[g][m] = T::mfma32(vf, pf[g][b], o[g][m]);
-          }
-        return;
+          for (int i = 0; i < 16; ++i) o[g][m][i] *= alpha;
       }
-      // the lane's keys: accumulator 8 b + e is key p0 + 16 b + 8 hf + e
-      auto key = [&](int i) { return p0 + 16 * (i / 8) + 8 * hf + i % 8; };
-      const uint32_t bad = (gone >> (8 * hf) & 0xFFu) | (gone >> (8 + 8 * hf) & 0xFF00u);
-      bool seen = false;
+      const float base = ref[g] == -INFINITY ? 0.f : ref[g];
 #pragma unroll
-      for (int g = 0; g < NG; ++g)
+      for (int w = 0; w < 8; ++w) {
+        const float pa = __builtin_amdgcn_exp2f(fmaf(s[g][2 * w], sc, -base));
+        const float pb = __builtin_amdgcn_exp2f(fmaf(s[g][2 * w + 1], sc, -base));
+        sum[g] += pa + pb;
+        pf[g][w / 4][w % 4] = T::pack2(pa, pb);
+      }
+    }
+  };
+  // the block at S (K's rows; V's KV bytes behind), from key p0 on; gone: its keys on bad pages
+  auto block = [&](const char* S, int p0, uint32_t gone) {
+    f32x16 s[NG];
+    u32x4 pf[NG][2];
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const bool in = key(i) >= klo[g] && key(i) < khi[g];
-          if (!in || (bad >> i & 1)) s[g][i] = -INFINITY;
-          seen |= in && there[g] && (bad >> i & 1);
-        }
-      if (seen && a.p.status) sync_or(a.p.status, VT_PAGED_BAD_PAGE);
+    for (int g = 0; g < NG; ++g) s[g] = f32x16{};
+#pragma unroll
+    for (int c = 0; c < NK; ++c) {
+      const u32x4 kf = *reinterpret_cast<const u32x4*>(S + (kr * D * 2 + ((2 * c + hf) ^ (kr % CPR)) * 16));
+#pragma unroll
+      for (int g = 0; g < NG; ++g) s[g] = T::mfma32(kf, qf[g][c], s[g]);
+    }
+    auto vfrag = [&](int m, int b) {
+      u32x4 f;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int r = vkey + 4 * h;
+        const u32x2 x = lds_read_tr(S + KV + 16 * b * D * 2 +
+                                    (r * D * 2 + ((4 * m + vdim) ^ (2 * (r % (CPR / 2)))) * 16 + (jl % 2) * 8));
+        f[2 * h] = x[0];
+        f[2 * h + 1] = x[1];
+      }
+      return f;
+    };
+    if (p0 >= full_lo && p0 + 32 <= full_hi && gone == 0) {  // all rows of the wave see all of it
       weigh(s, pf);
-      // values that no row of the wave sees stay out of the product even if they are
-      // infinite; where some rows see an infinite or NaN value and others do not, each row
-      // gets a product of its own
 #pragma unroll
       for (int m = 0; m < NM; ++m)
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
-          u32x4 vf = vfrag(m, b);
-          bool odd = false;
+          const u32x4 vf = vfrag(m, b);
 #pragma unroll
-          for (int e = 0; e < 8; ++e)
-            if (key(8 * b + e) < any_lo || key(8 * b + e) >= any_hi || (bad >> (8 * b + e) & 1))
-              vf[e / 2] &= e % 2 ? 0x0000FFFFu : 0xFFFF0000u;
-#pragma unroll
-          for (int w = 0; w < 4; ++w) odd |= odd2<T>(vf[w]);
-          const bool some = __builtin_amdgcn_ballot_w64(odd) != 0;
-#pragma unroll
-          for (int g = 0; g < NG; ++g) {
-            if (!some) {
-              o[g][m] = T::mfma32(vf, pf[g][b], o[g][m]);
-              continue;
-            }
-            f32x16 keep = o[g][m];
-#pragma unroll 1
-            for (int c = 0; c < 32; ++c) {
-              const int lo_c = __builtin_amdgcn_readlane(klo[g], c), hi_c = __builtin_amdgcn_readlane(khi[g], c);
-              u32x4 z = vf;
-#pragma unroll
-              for (int e = 0; e < 8; ++e)
-                if (key(8 * b + e) < lo_c || key(8 * b + e) >= hi_c) z[e / 2] &= e % 2 ? 0x0000FFFFu : 0xFFFF0000u;
-              const f32x16 r = T::mfma32(z, pf[g][b], o[g][m]);
-              if (ql == c) keep = r;
-            }
-            o[g][m] = keep;
-          }
+          for (int g = 0; g < NG; ++g) o[g][m] = T::mfma32(vf, pf[g][b], o[g][m]);
         }
-    };
-
-    if (stages > 0) {
-      // the query loads are waited for here, not among the stages' loads
-#pragma unroll
-      for (int g = 0; g < NG; ++g)
-#pragma unroll
-        for (int c = 0; c < NK; ++c) asm volatile("" : "+v"(qf[g][c]));
-      look(0);
-      fetch(0);
-      look(1);
-      widen(0);
-      for (int st = 0; st < stages; ++st) {
-        // this stage has landed, everywhere after the barrier; the other one is free
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-        __builtin_amdgcn_s_barrier();
-        asm volatile("" ::: "memory");
-        if (st + 1 < stages) fetch(st + 1);
-        look(st + 2);
-        const char* S = smem + (st % C::NST) * C::STAGE;
-        const int p0 = (b0 + st) * KS;
-#pragma unroll 1
-        for (int i = kg; i < 2; i += KG) {
-          const int k0 = p0 + 32 * i;
-          const uint32_t gone = __builtin_amdgcn_readfirstlane(absent[st % C::NST][i]);
-          if (k0 >= any_hi || k0 + 32 <= any_lo) continue;  // no row of this wave sees any of it
-          block(S + i * 32 * D * 2, k0, gone);
-        }
-        if (st + 1 < stages) widen(st + 1);
-      }
+      return;
     }
+    // the lane's keys: accumulator 8 b + e is key p0 + 16 b + 8 hf + e
+    auto key = [&](int i) { return p0 + 16 * (i / 8) + 8 * hf + i % 8; };
+    const uint32_t bad = (gone >> (8 * hf) & 0xFFu) | (gone >> (8 + 8 * hf) & 0xFF00u);
+    bool seen = false;
 #pragma unroll
-    for (int g = 0; g < NG; ++g) sum[g] += __shfl_xor(sum[g], 32, kWave);
-
-    if constexpr (KG == 2) {
-      // the second half of the waves leave their results in LDS, in register order
-      __syncthreads();
-      float* part = reinterpret_cast<float*>(smem) + wr * (NG * (D / 2 + 2)) * kWave + lane;
+    for (int g = 0; g < NG; ++g)
 #pragma unroll
-      for (int g = 0; g < NG; ++g) {
-        float* mine = part + g * (D / 2 + 2) * kWave;
-        if (kg == 1) {
-#pragma unroll
-          for (int m = 0; m < NM; ++m)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) mine[(m * 16 + i) * kWave] = o[g][m][i];
-          mine[(D / 2) * kWave] = ref[g];
-          mine[(D / 2 + 1) * kWave] = sum[g];
-        }
+      for (int i = 0; i < 16; ++i) {
+        const bool in = key(i) >= klo[g] && key(i) < khi[g];
+        if (!in || (bad >> i & 1)) s[g][i] = -INFINITY;
+        seen |= in && there[g] && (bad >> i & 1);
       }
-      __syncthreads();
+    if (seen && a.p.status) sync_or(a.p.status, VT_PAGED_BAD_PAGE);
+    weigh(s, pf);
+    // values that no row of the wave sees stay out of the product even if they are
+    // infinite; where some rows see an infinite or NaN value and others do not, each row
+    // gets a product of its own
 #pragma unroll
-      for (int g = 0; g < NG; ++g) {
-        const float* other = part + g * (D / 2 + 2) * kWave;
-        if (kg == 0) {
-          const float r1 = other[(D / 2) * kWave], top = fmaxf(ref[g], r1), base = top == -INFINITY ? 0.f : top;
-          const float f0 = __builtin_amdgcn_exp2f(ref[g] - base), f1 = __builtin_amdgcn_exp2f(r1 - base);
-          sum[g] = sum[g] * f0 + other[(D / 2 + 1) * kWave] * f1;
-          ref[g] = top;
+    for (int m = 0; m < NM; ++m)
 #pragma unroll
-          for (int m = 0; m < NM; ++m)
+      for (int b = 0; b < 2; ++b) {
+        u32x4 vf = vfrag(m, b);
+        bool odd = false;
 #pragma unroll
-            for (int i = 0; i < 16; ++i) o[g][m][i] = o[g][m][i] * f0 + other[(m * 16 + i) * kWave] * f1;
-        }
-      }
-    }
-
-    bool finish = true;
-    if (it.pieces > 1) {
-      const rsrc_t ru = make_rsrc(reinterpret_cast<char*>(a.part) + static_cast<int64_t>(it.slot) * C::PART,
-                                  it.pieces * C::PART);
-      // of this lane: quad i at 1 KiB steps, then (reference, sum) per group
-      const uint32_t at = (wr * (C::QUADS * 16 + NG * 8)) * kWave;
-      auto quad = [&](int i) { return at + i * 16 * kWave + lane * 16; };
-      auto stats = [&](int g) { return at + C::QUADS * 16 * kWave + g * 8 * kWave + lane * 8; };
-      if (kg == 0) {
-        const uint32_t mine = it.piece * C::PART;
+        for (int e = 0; e < 8; ++e)
+          if (key(8 * b + e) < any_lo || key(8 * b + e) >= any_hi || (bad >> (8 * b + e) & 1))
+            vf[e / 2] &= e % 2 ? 0x0000FFFFu : 0xFFFF0000u;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) odd |= odd2<T>(vf[w]);
+        const bool some = __builtin_amdgcn_ballot_w64(odd) != 0;
 #pragma unroll
         for (int g = 0; g < NG; ++g) {
+          if (!some) {
+            o[g][m] = T::mfma32(vf, pf[g][b], o[g][m]);
+            continue;
+          }
+          f32x16 keep = o[g][m];
+#pragma unroll 1
+          for (int c = 0; c < 32; ++c) {
+            const int lo_c = __builtin_amdgcn_readlane(klo[g], c), hi_c = __builtin_amdgcn_readlane(khi[g], c);
+            u32x4 z = vf;
 #pragma unroll
-          for (int m = 0; m < NM; ++m)
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-              __builtin_amdgcn_raw_buffer_store_b128(
-                  __builtin_bit_cast(u32x4, f32x4{o[g][m][4 * i], o[g][m][4 * i + 1], o[g][m][4 * i + 2], o[g][m][4 * i + 3]}),
-                  ru, mine + quad((g * NM + m) * 4 + i), 0, kCoherent);
-          __builtin_amdgcn_raw_buffer_store_b64(
-              u32x2{__builtin_bit_cast(uint32_t, ref[g]), __builtin_bit_cast(uint32_t, sum[g])}, ru, mine + stats(g), 0,
-              kCoherent);
+            for (int e = 0; e < 8; ++e)
+              if (key(8 * b + e) < lo_c || key(8 * b + e) >= hi_c) z[e / 2] &= e % 2 ? 0x0000FFFFu : 0xFFFF0000u;
+            const f32x16 r = T::mfma32(z, pf[g][b], o[g][m]);
+            if (ql == c) keep = r;
+          }
+          o[g][m] = keep;
         }
       }
-      mem_done();
-      __syncthreads();
-      if (threadIdx.x == 0)
-        lds[0] = __hip_atomic_fetch_add(a.arrived + it.unit, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) ==
-                 static_cast<uint32_t>(it.pieces - 1);
-      __syncthreads();
-      // the last piece to arrive joins them all, in their order
-      finish = lds[0] != 0;
-      if (finish) {
-        if (threadIdx.x == 0) sync_store(a.arrived + it.unit, 0u);
-        if (kg == 0) {
+  };
+
+  if (stages > 0) {
+    // the query loads are waited for here, not among the stages' loads
 #pragma unroll
-          for (int g = 0; g < NG; ++g) {
-            float top = -INFINITY;
-            for (int c = 0; c < it.pieces; ++c) top = fmaxf(top, buf_ld_shared(ru, c * C::PART + stats(g)));
-            ref[g] = top;
-            sum[g] = 0.f;
+    for (int g = 0; g < NG; ++g)
 #pragma unroll
-            for (int m = 0; m < NM; ++m) o[g][m] = f32x16{};
-          }
-          for (int c = 0; c < it.pieces; ++c) {
+      for (int c = 0; c < NK; ++c) asm volatile("" : "+v"(qf[g][c]));
+    look(0);
+    fetch(0);
+    look(1);
+    widen(0);
+    for (int st = 0; st < stages; ++st) {
+      // this stage has landed, everywhere after the barrier; the other one is free
+      asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+      __builtin_amdgcn_s_barrier();
+      asm volatile("" ::: "memory");
+      if (st + 1 < stages) fetch(st + 1);
+      look(st + 2);
+      const char* S = smem + (st % C::NST) * C::STAGE;
+      const int p0 = (b0 + st) * KS;
+#pragma unroll 1
+      for (int i = kg; i < 2; i += KG) {
+        const int k0 = p0 + 32 * i;
+        const uint32_t gone = __builtin_amdgcn_readfirstlane(absent[st % C::NST][i]);
+        if (k0 >= any_hi || k0 + 32 <= any_lo) continue;  // no row of this wave sees any of it
+        block(S + i * 32 * D * 2, k0, gone);
+      }
+      if (st + 1 < stages) widen(st + 1);
+    }
+  }
 #pragma unroll
-            for (int g = 0; g < NG; ++g) {
-              float r, t;
-              buf_ld_shared2(ru, c * C::PART + stats(g), r, t);
-              u32x4 x[NM * 4];
+  for (int g = 0; g < NG; ++g) sum[g] += __shfl_xor(sum[g], 32, kWave);
+
+  if constexpr (KG == 2) {
+    // the second half of the waves leave their results in LDS, in register order
+    __syncthreads();
+    float* part = reinterpret_cast<float*>(smem) + wr * (NG * (D / 2 + 2)) * kWave + lane;
 #pragma unroll
-              for (int i = 0; i < NM * 4; ++i)
-                x[i] = __builtin_amdgcn_raw_buffer_load_b128(ru, c * C::PART + quad(g * NM * 4 + i), 0, kCoherent);
-              const float f = r == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(r - ref[g]);
-              sum[g] += f * t;
+    for (int g = 0; g < NG; ++g) {
+      float* mine = part + g * (D / 2 + 2) * kWave;
+      if (kg == 1) {
 #pragma unroll
-              for (int i = 0; i < NM * 4; ++i)
+        for (int m = 0; m < NM; ++m)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) o[g][i / 4][i % 4 * 4 + e] += f * __builtin_bit_cast(f32x4, x[i])[e];
-            }
-          }
-        }
+          for (int i = 0; i < 16; ++i) mine[(m * 16 + i) * kWave] = o[g][m][i];
+        mine[(D / 2) * kWave] = ref[g];
+        mine[(D / 2 + 1) * kWave] = sum[g];
       }
     }
-    if (finish && kg == 0) {
-      const float vs = F8 && a.p.v_scale ? a.p.v_scale[it.head] : 1.f;
+    __syncthreads();
+#pragma unroll
+    for (int g = 0; g < NG; ++g) {
+      const float* other = part + g * (D / 2 + 2) * kWave;
+      if (kg == 0) {
+        const float r1 = other[(D / 2) * kWave], top = fmaxf(ref[g], r1), base = top == -INFINITY ? 0.f : top;
+        const float f0 = __builtin_amdgcn_exp2f(ref[g] - base), f1 = __builtin_amdgcn_exp2f(r1 - base);
+        sum[g] = sum[g] * f0 + other[(D / 2 + 1) * kWave] * f1;
+        ref[g] = top;
+#pragma unroll
+        for (int m = 0; m < NM; ++m)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) o[g][m][i] = o[g][m][i] * f0 + other[(m * 16 + i) * kWave] * f1;
+      }
+    }
+  }
+
+  bool finish = true;
+  if (it.pieces > 1) {
+    const rsrc_t ru = make_rsrc(reinterpret_cast<char*>(a.part) + static_cast<int64_t>(it.slot) * C::PART,
+                                it.pieces * C::PART);
+    // of this lane: quad i at 1 KiB steps, then (reference, sum) per group
+    const uint32_t at = (wr * (C::QUADS * 16 + NG * 8)) * kWave;
+    auto quad = [&](int i) { return at + i * 16 * kWave + lane * 16; };
+    auto stats = [&](int g) { return at + C::QUADS * 16 * kWave + g * 8 * kWave + lane * 8; };
+    if (kg == 0) {
+      const uint32_t mine = it.piece * C::PART;
 #pragma unroll
       for (int g = 0; g < NG; ++g) {
-        if (!there[g]) continue;
-        const int tok = row[g] / a.group, hd = it.head * a.group + row[g] - tok * a.group;
-        const float inv = sum[g] == 0.f ? 0.f : vs / sum[g];
-        uint16_t* op = a.out + (q.b + tok) * a.ld_out + static_cast<int64_t>(hd) * D + 4 * hf;
-        // accumulator i of tile m is element 32 m + 8 (i / 4) + 4 hf + i % 4
 #pragma unroll
         for (int m = 0; m < NM; ++m)
 #pragma unroll
           for (int i = 0; i < 4; ++i)
-            *reinterpret_cast<u32x2*>(op + 32 * m + 8 * i) =
-                u32x2{T::pack2(o[g][m][4 * i] * inv, o[g][m][4 * i + 1] * inv),
-                      T::pack2(o[g][m][4 * i + 2] * inv, o[g][m][4 * i + 3] * inv)};
-        if (a.lse && hf == 0)
-          a.lse[static_cast<int64_t>(q.b + tok) * a.n_q + hd] =
-              sum[g] == 0.f ? -INFINITY : (ref[g] + __builtin_amdgcn_logf(sum[g])) * 0.6931471805599453f;
+            __builtin_amdgcn_raw_buffer_store_b128(
+                __builtin_bit_cast(u32x4, f32x4{o[g][m][4 * i], o[g][m][4 * i + 1], o[g][m][4 * i + 2], o[g][m][4 * i + 3]}),
+                ru, mine + quad((g * NM + m) * 4 + i), 0, kCoherent);
+        __builtin_amdgcn_raw_buffer_store_b64(
+            u32x2{__builtin_bit_cast(uint32_t, ref[g]), __builtin_bit_cast(uint32_t, sum[g])}, ru, mine + stats(g), 0,
+            kCoherent);
       }
     }
-    __syncthreads();  // the stages are free for the next item
+    mem_done();
+    __syncthreads();
+    if (threadIdx.x == 0)
+      lds[0] = __hip_atomic_fetch_add(a.arrived + it.unit, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) ==
+               static_cast<uint32_t>(it.pieces - 1);
+    __syncthreads();
+    // the last piece to arrive joins them all, in their order
+    finish = lds[0] != 0;
+    if (finish) {
+      if (threadIdx.x == 0) sync_store(a.arrived + it.unit, 0u);
+      if (kg == 0) {
+#pragma unroll
+        for (int g = 0; g < NG; ++g) {
+          ref[g] = -INFINITY;
+          sum[g] = 0.f;
+#pragma unroll
+          for (int m = 0; m < NM; ++m) o[g][m] = f32x16{};
+        }
+        for (int c = 0; c < it.pieces; ++c) {
+          u32x4 y[NG][NM * 4];
+          float yr[NG], yt[NG];
+#pragma unroll
+          for (int g = 0; g < NG; ++g) {
+            buf_ld_shared2(ru, c * C::PART + stats(g), yr[g], yt[g]);
+#pragma unroll
+            for (int i = 0; i < NM * 4; ++i)
+              y[g][i] = __builtin_amdgcn_raw_buffer_load_b128(ru, c * C::PART + quad(g * NM * 4 + i), 0, kCoherent);
+          }
+#pragma unroll
+          for (int g = 0; g < NG; ++g) {
+            const float top = fmaxf(ref[g], yr[g]), base = top == -INFINITY ? 0.f : top;
+            const float f0 = __builtin_amdgcn_exp2f(ref[g] - base), f1 = __builtin_amdgcn_exp2f(yr[g] - base);
+            ref[g] = top;
+            sum[g] = sum[g] * f0 + yt[g] * f1;
+#pragma unroll
+            for (int i = 0; i < NM * 4; ++i)
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                o[g][i / 4][i % 4 * 4 + e] =
+                    o[g][i / 4][i % 4 * 4 + e] * f0 + f1 * __builtin_bit_cast(f32x4, y[g][i])[e];
+          }
+        }
+      }
+    }
+  }
+  if (finish && kg == 0) {
+    const float vs = F8 && a.p.v_scale ? a.p.v_scale[it.head] : 1.f;
+#pragma unroll
+    for (int g = 0; g < NG; ++g) {
+      if (!there[g]) continue;
+      const int tok = row[g] / a.group, hd = it.head * a.group + row[g] - tok * a.group;
+      const float inv = sum[g] == 0.f ? 0.f : vs / sum[g];
+      uint16_t* op = a.out + (q.b + tok) * a.ld_out + static_cast<int64_t>(hd) * D + 4 * hf;
+      // accumulator i of tile m is element 32 m + 8 (i / 4) + 4 hf + i % 4
+#pragma unroll
+      for (int m = 0; m < NM; ++m)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          *reinterpret_cast<u32x2*>(op + 32 * m + 8 * i) =
+              u32x2{T::pack2(o[g][m][4 * i] * inv, o[g][m][4 * i + 1] * inv),
+                    T::pack2(o[g][m][4 * i + 2] * inv, o[g][m][4 * i + 3] * inv)};
+      if (a.lse && hf == 0)
+        a.lse[static_cast<int64_t>(q.b + tok) * a.n_q + hd] =
+            sum[g] == 0.f ? -INFINITY : (ref[g] + __builtin_amdgcn_logf(sum[g])) * 0.6931471805599453f;
+    }
   }
 }
 
@@ -565,12 +566,9 @@ hipError_t launch_chunk(const AttnArgs& a, int type, bool f8, int head_dim, int 
   auto pick1 = [&](auto X) { return f8 ? pick2(X, std::true_type{}) : pick2(X, std::false_type{}); };
   auto* kernel = type == VT_T_F16 ? pick1(Half{}) : pick1(BFloat{});
   const int64_t tiles = static_cast<int64_t>(a.n_tok) * a.group / rows + a.p.n_seqs;
-  const int64_t units = tiles * a.p.n_kv, blocks = (static_cast<int64_t>(a.p.capacity) + KS - 1) / KS;
-  const int64_t items = std::min(units * blocks, units + 2 * static_cast<int64_t>(a.target));
   hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, shared);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(kernel, dim3(static_cast<uint32_t>(std::max<int64_t>(1, std::min<int64_t>(items, 16384)))), dim3(CTH),
-                     shared, s, a);
+  hipLaunchKernelGGL(kernel, dim3(grid_of(a, tiles, KS)), dim3(CTH), shared, s, a);
   return hipGetLastError();
 }
 
