@@ -1,8 +1,7 @@
 // Attention of many query rows over a paged cache: chunks of prompts.
 //
 // A workgroup of four waves takes a tile of rows of one KV head (a row is one query
-// head of one token, the heads that share the KV head side by side), a wave NG groups
-// of 32 rows. Keys and values come in stages of 64 into LDS, once for all rows of
+// head of one token, the heads that share the KV head side by side), a wave 32 rows. Keys and values come in stages of 64 into LDS, once for all rows of
 // the tile: 16-bit caches straight from memory, 8-bit ones through registers, where
 // they are widened. Both products run as
 //   S^T = K Q^T, O^T = V^T P^T on 32 x 32 x 16 matrix instructions:
@@ -62,23 +61,22 @@ __device__ __forceinline__ void dma_lanes(uint32_t to, const char* p) {
 
 __device__ __forceinline__ int swap_bits23(int r) { return (r & ~12) | ((r & 4) << 1) | ((r & 8) >> 1); }
 
-// NG groups of 32 rows per wave; KG groups of waves share the rows and take every KG-th
-// block of 32 keys.
-template <int D, int NG, int KG>
+// KG groups of waves share the rows and take every KG-th block of 32 keys.
+template <int D, int KG>
 struct Chunk {
   static constexpr int RGW = CW / KG;           // waves side by side over the rows
-  static constexpr int ROWS = RGW * NG * 32;
+  static constexpr int ROWS = RGW * 32;
   static constexpr int STAGE = KS * D * 2 * 2;  // bytes of a stage: K, then V
   static constexpr int NST = 2;
   static constexpr int LDS = STAGE * NST;
-  // a partial result: [wave][register quad][lane][4], then references and sums [wave][group][lane]
-  static constexpr int QUADS = NG * D / 8;
-  static constexpr uint32_t PART = RGW * kWave * (QUADS * 16 + NG * 8);
+  // a partial result of a wave: [register quad][lane][4], then a reference and a sum per lane
+  static constexpr int QUADS = D / 8;
+  static constexpr uint32_t PART = RGW * kWave * (QUADS * 16 + 8);
 };
 
-template <class T, bool F8, int D, bool BIG, int NG, int KG>
-__global__ void __launch_bounds__(CTH, NG == 1 ? 2 : 1) attn_chunk_kernel(AttnArgs a) {
-  using C = Chunk<D, NG, KG>;
+template <class T, bool F8, int D, bool BIG, int KG>
+__global__ void __launch_bounds__(CTH, 2) attn_chunk_kernel(AttnArgs a) {
+  using C = Chunk<D, KG>;
   using P = Plan<C::ROWS, KS, CTH>;
   constexpr int NK = D / 16, NM = D / 32, CPR = D / 8;
   constexpr int KV = KS * D * 2;  // bytes of a stage's K
@@ -98,22 +96,14 @@ __global__ void __launch_bounds__(CTH, NG == 1 ? 2 : 1) attn_chunk_kernel(AttnAr
   if (!next_item<P>(a, blockIdx.x, it, lds)) return;
   const Seq& q = it.q;
   const int rows = q.nt * a.group;
-  int row[NG], khi[NG], klo[NG];
-  bool there[NG];
-  int full_hi = INT32_MAX, any_hi = INT32_MIN, full_lo = INT32_MIN, any_lo = INT32_MAX;
-#pragma unroll
-  for (int g = 0; g < NG; ++g) {
-    const int r = it.tile * C::ROWS + (wr * NG + g) * 32 + ql;
-    there[g] = r < rows;
-    row[g] = min(r, rows - 1);
-    const int pos = q.pos0 + row[g] / a.group;
-    khi[g] = min(pos + 1, q.keys);
-    klo[g] = a.window > 0 ? max(pos, 0) - (a.window - 1) : 0;
-    full_hi = min(full_hi, khi[g]);
-    any_hi = max(any_hi, khi[g]);
-    full_lo = max(full_lo, klo[g]);
-    any_lo = min(any_lo, klo[g]);
-  }
+  const int r0 = it.tile * C::ROWS + wr * 32 + ql, row = min(r0, rows - 1);
+  const bool there = r0 < rows;
+  const int tok = row / a.group, head = it.head * a.group + row - tok * a.group;
+  const int pos = q.pos0 + tok;  // its keys: klo <= p < khi
+  const int khi = min(pos + 1, q.keys), klo = a.window > 0 ? max(pos, 0) - (a.window - 1) : 0;
+  // keys that every row of the wave sees lie in full_lo .. full_hi - 1, those of any row in any_lo ..
+  // any_hi - 1
+  int full_hi = khi, any_hi = khi, full_lo = klo, any_lo = klo;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
     full_hi = min(full_hi, __shfl_xor(full_hi, o, kWave));
@@ -141,25 +131,18 @@ __global__ void __launch_bounds__(CTH, NG == 1 ? 2 : 1) attn_chunk_kernel(AttnAr
   const int32_t* tabv = a.p.table + it.s * a.p.ld_table;
   ConstInt* tab = constant(tabv);
 
-  u32x4 qf[NG][NK];
+  u32x4 qf[NK];
+  {
+    const uint16_t* qp = a.q + (q.b + tok) * a.ld_q + static_cast<int64_t>(head) * D;
 #pragma unroll
-  for (int g = 0; g < NG; ++g) {
-    const int tok = row[g] / a.group, j = row[g] - tok * a.group;
-    const uint16_t* qp = a.q + (q.b + tok) * a.ld_q + (static_cast<int64_t>(it.head) * a.group + j) * D;
-#pragma unroll
-    for (int c = 0; c < NK; ++c) qf[g][c] = load16(qp + c * 16 + 8 * hf);
+    for (int c = 0; c < NK; ++c) qf[c] = load16(qp + c * 16 + 8 * hf);
   }
   const float sc = a.scale2 * (F8 && a.p.k_scale ? a.p.k_scale[it.head] : 1.f);
 
-  f32x16 o[NG][NM];
-  float ref[NG], sum[NG];
+  f32x16 o[NM];
+  float ref = -INFINITY, sum = 0.f;
 #pragma unroll
-  for (int g = 0; g < NG; ++g) {
-    ref[g] = -INFINITY;
-    sum[g] = 0.f;
-#pragma unroll
-    for (int m = 0; m < NM; ++m) o[g][m] = f32x16{};
-  }
+  for (int m = 0; m < NM; ++m) o[m] = f32x16{};
 
   // ---- stages into LDS -------------------------------------------------------
   // A stage's page numbers are looked up a stage ahead of its loads. IDS: those a
@@ -201,10 +184,9 @@ __global__ void __launch_bounds__(CTH, NG == 1 ? 2 : 1) attn_chunk_kernel(AttnAr
       }
       if (F8 || u == LPW - 1) {
         char* flag = reinterpret_cast<char*>(absent[st % C::NST]) + (F8 ? first_row(u) : wave * 16) / 8;
-        if (lane == 0) {
-          if (F8 && RPL == 8) *reinterpret_cast<uint8_t*>(flag) = static_cast<uint8_t>(gone);
-          else *reinterpret_cast<uint16_t*>(flag) = static_cast<uint16_t>(gone);
-        }
+        // (every lane stores it: a branch that lanes take apart would cost the stages' loop its plain flow)
+        if (F8 && RPL == 8) *reinterpret_cast<uint8_t*>(flag) = static_cast<uint8_t>(gone);
+        else *reinterpret_cast<uint16_t*>(flag) = static_cast<uint16_t>(gone);
         gone = 0;
       }
       const int r0 = first_row(u), r = r0 + lrow;
@@ -266,84 +248,72 @@ __global__ void __launch_bounds__(CTH, NG == 1 ? 2 : 1) attn_chunk_kernel(AttnAr
   const int grp = lane / 16, jl = lane % 16;
   const int vkey = 8 * (grp / 2) + jl / 4, vdim = 2 * (grp % 2) + (jl % 4) / 2;
   const int kr = swap_bits23(ql);
-  // scores to weights, sums and the second product's operand
-  auto weigh = [&](f32x16 (&s)[NG], u32x4 (&pf)[NG][2]) {
+  // A lane's parts of a block at S: chunk c of its key, and element 32 m + l % 32 of keys
+  // 16 b + 8 hf .. + 7.
+  auto kfrag = [&](const char* S, int c) {
+    return *reinterpret_cast<const u32x4*>(S + (kr * D * 2 + ((2 * c + hf) ^ (kr % CPR)) * 16));
+  };
+  auto vfrag = [&](const char* S, int m, int b) {
+    u32x4 f;
 #pragma unroll
-    for (int g = 0; g < NG; ++g) {
-      float top = s[g][0];
+    for (int h = 0; h < 2; ++h) {
+      const int r = vkey + 4 * h;
+      const u32x2 x = lds_read_tr(S + KV + 16 * b * D * 2 +
+                                  (r * D * 2 + ((4 * m + vdim) ^ (2 * (r % (CPR / 2)))) * 16 + (jl % 2) * 8));
+      f[2 * h] = x[0];
+      f[2 * h + 1] = x[1];
+    }
+    return f;
+  };
+  // the largest of a lane's scores, in units of the weights' exponents
+  auto largest = [&](const f32x16& s) {
+    float top = s[0];
 #pragma unroll
-      for (int i = 1; i < 16; ++i) top = fmaxf(top, s[g][i]);
-      top *= sc;
-      if (__builtin_amdgcn_ballot_w64(top > ref[g] + 8.f) != 0) {
-        top = fmaxf(top, __shfl_xor(top, 32, kWave));
-        const float next = fmaxf(top, ref[g]);
-        const float alpha = next == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ref[g] - next);
-        ref[g] = next;
-        sum[g] *= alpha;
+    for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
+    return top * sc;
+  };
+  // a new reference for the rows: the largest score so far
+  auto refer = [&](float top) {
+    top = fmaxf(top, __shfl_xor(top, 32, kWave));
+    const float next = fmaxf(top, ref);
+    const float alpha = next == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ref - next);
+    ref = next;
+    sum *= alpha;
 #pragma unroll
-        for (int m = 0; m < NM; ++m)
+    for (int m = 0; m < NM; ++m)
 #pragma unroll
-          for (int i = 0; i < 16; ++i) o[g][m][i] *= alpha;
-      }
-      const float base = ref[g] == -INFINITY ? 0.f : ref[g];
+      for (int i = 0; i < 16; ++i) o[m][i] *= alpha;
+  };
+  // scores to weights, the second product's operand, and their sum
+  auto weigh = [&](const f32x16& s, u32x4 (&pf)[2]) {
+    const float base = ref == -INFINITY ? 0.f : ref;
 #pragma unroll
-      for (int w = 0; w < 8; ++w) {
-        const float pa = __builtin_amdgcn_exp2f(fmaf(s[g][2 * w], sc, -base));
-        const float pb = __builtin_amdgcn_exp2f(fmaf(s[g][2 * w + 1], sc, -base));
-        sum[g] += pa + pb;
-        pf[g][w / 4][w % 4] = T::pack2(pa, pb);
-      }
+    for (int w = 0; w < 8; ++w) {
+      const float pa = __builtin_amdgcn_exp2f(fmaf(s[2 * w], sc, -base));
+      const float pb = __builtin_amdgcn_exp2f(fmaf(s[2 * w + 1], sc, -base));
+      sum += pa + pb;
+      pf[w / 4][w % 4] = T::pack2(pa, pb);
     }
   };
-  // the block at S (K's rows; V's KV bytes behind), from key p0 on; gone: its keys on bad pages
-  auto block = [&](const char* S, int p0, uint32_t gone) {
-    f32x16 s[NG];
-    u32x4 pf[NG][2];
+  // A block that some rows of the wave do not see whole, from key p0 on; gone: its keys on
+  // bad pages.
+  auto partly = [&](const char* S, int p0, uint32_t gone) {
+    f32x16 s = f32x16{};
 #pragma unroll
-    for (int g = 0; g < NG; ++g) s[g] = f32x16{};
-#pragma unroll
-    for (int c = 0; c < NK; ++c) {
-      const u32x4 kf = *reinterpret_cast<const u32x4*>(S + (kr * D * 2 + ((2 * c + hf) ^ (kr % CPR)) * 16));
-#pragma unroll
-      for (int g = 0; g < NG; ++g) s[g] = T::mfma32(kf, qf[g][c], s[g]);
-    }
-    auto vfrag = [&](int m, int b) {
-      u32x4 f;
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int r = vkey + 4 * h;
-        const u32x2 x = lds_read_tr(S + KV + 16 * b * D * 2 +
-                                    (r * D * 2 + ((4 * m + vdim) ^ (2 * (r % (CPR / 2)))) * 16 + (jl % 2) * 8));
-        f[2 * h] = x[0];
-        f[2 * h + 1] = x[1];
-      }
-      return f;
-    };
-    if (p0 >= full_lo && p0 + 32 <= full_hi && gone == 0) {  // all rows of the wave see all of it
-      weigh(s, pf);
-#pragma unroll
-      for (int m = 0; m < NM; ++m)
-#pragma unroll
-        for (int b = 0; b < 2; ++b) {
-          const u32x4 vf = vfrag(m, b);
-#pragma unroll
-          for (int g = 0; g < NG; ++g) o[g][m] = T::mfma32(vf, pf[g][b], o[g][m]);
-        }
-      return;
-    }
+    for (int c = 0; c < NK; ++c) s = T::mfma32(kfrag(S, c), qf[c], s);
     // the lane's keys: accumulator 8 b + e is key p0 + 16 b + 8 hf + e
     auto key = [&](int i) { return p0 + 16 * (i / 8) + 8 * hf + i % 8; };
     const uint32_t bad = (gone >> (8 * hf) & 0xFFu) | (gone >> (8 + 8 * hf) & 0xFF00u);
     bool seen = false;
 #pragma unroll
-    for (int g = 0; g < NG; ++g)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const bool in = key(i) >= klo[g] && key(i) < khi[g];
-        if (!in || (bad >> i & 1)) s[g][i] = -INFINITY;
-        seen |= in && there[g] && (bad >> i & 1);
-      }
-    if (seen && a.p.status) sync_or(a.p.status, VT_PAGED_BAD_PAGE);
+    for (int i = 0; i < 16; ++i) {
+      const bool in = key(i) >= klo && key(i) < khi;
+      if (!in || (bad >> i & 1)) s[i] = -INFINITY;
+      seen |= in && there && (bad >> i & 1);
+    }
+    if (__builtin_amdgcn_ballot_w64(seen) != 0 && a.p.status) sync_or(a.p.status, VT_PAGED_BAD_PAGE);
+    u32x4 pf[2];
+    refer(largest(s));
     weigh(s, pf);
     // values that no row of the wave sees stay out of the product even if they are
     // infinite; where some rows see an infinite or NaN value and others do not, each row
@@ -352,7 +322,7 @@ __global__ void __launch_bounds__(CTH, NG == 1 ? 2 : 1) attn_chunk_kernel(AttnAr
     for (int m = 0; m < NM; ++m)
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
-        u32x4 vf = vfrag(m, b);
+        u32x4 vf = vfrag(S, m, b);
         bool odd = false;
 #pragma unroll
         for (int e = 0; e < 8; ++e)
@@ -360,117 +330,132 @@ __global__ void __launch_bounds__(CTH, NG == 1 ? 2 : 1) attn_chunk_kernel(AttnAr
             vf[e / 2] &= e % 2 ? 0x0000FFFFu : 0xFFFF0000u;
 #pragma unroll
         for (int w = 0; w < 4; ++w) odd |= odd2<T>(vf[w]);
-        const bool some = __builtin_amdgcn_ballot_w64(odd) != 0;
-#pragma unroll
-        for (int g = 0; g < NG; ++g) {
-          if (!some) {
-            o[g][m] = T::mfma32(vf, pf[g][b], o[g][m]);
-            continue;
-          }
-          f32x16 keep = o[g][m];
-#pragma unroll 1
-          for (int c = 0; c < 32; ++c) {
-            const int lo_c = __builtin_amdgcn_readlane(klo[g], c), hi_c = __builtin_amdgcn_readlane(khi[g], c);
-            u32x4 z = vf;
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-              if (key(8 * b + e) < lo_c || key(8 * b + e) >= hi_c) z[e / 2] &= e % 2 ? 0x0000FFFFu : 0xFFFF0000u;
-            const f32x16 r = T::mfma32(z, pf[g][b], o[g][m]);
-            if (ql == c) keep = r;
-          }
-          o[g][m] = keep;
+        if (__builtin_amdgcn_ballot_w64(odd) == 0) {
+          o[m] = T::mfma32(vf, pf[b], o[m]);
+          continue;
         }
+        f32x16 keep = o[m];
+#pragma unroll 1
+        for (int c = 0; c < 32; ++c) {
+          const int lo_c = __builtin_amdgcn_readlane(klo, c), hi_c = __builtin_amdgcn_readlane(khi, c);
+          u32x4 z = vf;
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            if (key(8 * b + e) < lo_c || key(8 * b + e) >= hi_c) z[e / 2] &= e % 2 ? 0x0000FFFFu : 0xFFFF0000u;
+          const f32x16 r = T::mfma32(z, pf[b], o[m]);
+          if (ql == c) keep = r;
+        }
+        o[m] = keep;
       }
   };
 
   if (stages > 0) {
     // the query loads are waited for here, not among the stages' loads
 #pragma unroll
-    for (int g = 0; g < NG; ++g)
-#pragma unroll
-      for (int c = 0; c < NK; ++c) asm volatile("" : "+v"(qf[g][c]));
+    for (int c = 0; c < NK; ++c) asm volatile("" : "+v"(qf[c]));
     look(0);
     fetch(0);
     look(1);
-    widen(0);
-    for (int st = 0; st < stages; ++st) {
-      // this stage has landed, everywhere after the barrier; the other one is free
+    // Stage st: what was loaded has landed, everywhere after the barrier, and the stage
+    // before is done with; the next one sets out for its place.
+    int begun = -1;
+    auto begin = [&](int st) {
+      if (st == begun) return;
+      begun = st;
+      widen(st);
       asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
       __builtin_amdgcn_s_barrier();
       asm volatile("" ::: "memory");
       if (st + 1 < stages) fetch(st + 1);
       look(st + 2);
-      const char* S = smem + (st % C::NST) * C::STAGE;
-      const int p0 = (b0 + st) * KS;
-#pragma unroll 1
-      for (int i = kg; i < 2; i += KG) {
-        const int k0 = p0 + 32 * i;
-        const uint32_t gone = __builtin_amdgcn_readfirstlane(absent[st % C::NST][i]);
-        if (k0 >= any_hi || k0 + 32 <= any_lo) continue;  // no row of this wave sees any of it
-        block(S + i * 32 * D * 2, k0, gone);
+    };
+    // Blocks t of 32 keys: two of a stage, or (KG 2) the wave's own one. An inner loop for
+    // blocks that the wave's rows see whole, left at any other one and at one that
+    // raises a reference, which goes the general way: with these cases inside it the outputs
+    // moved between registers at every block.
+    constexpr int BPS = 2 / KG;
+    const int blocks = stages * BPS;
+    auto sub_of = [&](int t) { return KG == 2 ? kg : t % 2; };
+    auto first_key = [&](int t) { return (b0 + t / BPS) * KS + sub_of(t) * 32; };
+    auto place = [&](int t) { return smem + (t / BPS) % C::NST * C::STAGE + sub_of(t) * 32 * D * 2; };
+    int t = 0;
+    while (t < blocks) {
+      for (; t < blocks; ++t) {
+        const int k0 = first_key(t);
+        if (k0 < full_lo || k0 + 32 > full_hi) break;
+        begin(t / BPS);
+        if (__builtin_amdgcn_readfirstlane(absent[t / BPS % C::NST][sub_of(t)]) != 0) break;
+        const char* B = place(t);
+        // all fragments are on their way before the first is used: V's arrive behind the scores
+        u32x4 kf[NK], vf[NM][2], pf[2];
+#pragma unroll
+        for (int c = 0; c < NK; ++c) kf[c] = kfrag(B, c);
+#pragma unroll
+        for (int m = 0; m < NM; ++m)
+#pragma unroll
+          for (int b = 0; b < 2; ++b) vf[m][b] = vfrag(B, m, b);
+        __builtin_amdgcn_sched_barrier(0);
+        f32x16 s = f32x16{};
+#pragma unroll
+        for (int c = 0; c < NK; ++c) s = T::mfma32(kf[c], qf[c], s);
+        if (__builtin_amdgcn_ballot_w64(largest(s) > ref + 8.f) != 0) break;
+        weigh(s, pf);
+#pragma unroll
+        for (int m = 0; m < NM; ++m)
+#pragma unroll
+          for (int b = 0; b < 2; ++b) o[m] = T::mfma32(vf[m][b], pf[b], o[m]);
       }
-      if (st + 1 < stages) widen(st + 1);
+      if (t >= blocks) break;
+      begin(t / BPS);
+      const int k0 = first_key(t);
+      if (k0 < any_hi && k0 + 32 > any_lo)  // some row of this wave sees some of it
+        partly(place(t), k0, __builtin_amdgcn_readfirstlane(absent[t / BPS % C::NST][sub_of(t)]));
+      ++t;
     }
   }
-#pragma unroll
-  for (int g = 0; g < NG; ++g) sum[g] += __shfl_xor(sum[g], 32, kWave);
+  sum += __shfl_xor(sum, 32, kWave);
 
   if constexpr (KG == 2) {
     // the second half of the waves leave their results in LDS, in register order
     __syncthreads();
-    float* part = reinterpret_cast<float*>(smem) + wr * (NG * (D / 2 + 2)) * kWave + lane;
+    float* part = reinterpret_cast<float*>(smem) + wr * (D / 2 + 2) * kWave + lane;
+    if (kg == 1) {
 #pragma unroll
-    for (int g = 0; g < NG; ++g) {
-      float* mine = part + g * (D / 2 + 2) * kWave;
-      if (kg == 1) {
+      for (int m = 0; m < NM; ++m)
 #pragma unroll
-        for (int m = 0; m < NM; ++m)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) mine[(m * 16 + i) * kWave] = o[g][m][i];
-        mine[(D / 2) * kWave] = ref[g];
-        mine[(D / 2 + 1) * kWave] = sum[g];
-      }
+        for (int i = 0; i < 16; ++i) part[(m * 16 + i) * kWave] = o[m][i];
+      part[(D / 2) * kWave] = ref;
+      part[(D / 2 + 1) * kWave] = sum;
     }
     __syncthreads();
+    if (kg == 0) {
+      const float r1 = part[(D / 2) * kWave], top = fmaxf(ref, r1), base = top == -INFINITY ? 0.f : top;
+      const float f0 = __builtin_amdgcn_exp2f(ref - base), f1 = __builtin_amdgcn_exp2f(r1 - base);
+      sum = sum * f0 + part[(D / 2 + 1) * kWave] * f1;
+      ref = top;
 #pragma unroll
-    for (int g = 0; g < NG; ++g) {
-      const float* other = part + g * (D / 2 + 2) * kWave;
-      if (kg == 0) {
-        const float r1 = other[(D / 2) * kWave], top = fmaxf(ref[g], r1), base = top == -INFINITY ? 0.f : top;
-        const float f0 = __builtin_amdgcn_exp2f(ref[g] - base), f1 = __builtin_amdgcn_exp2f(r1 - base);
-        sum[g] = sum[g] * f0 + other[(D / 2 + 1) * kWave] * f1;
-        ref[g] = top;
+      for (int m = 0; m < NM; ++m)
 #pragma unroll
-        for (int m = 0; m < NM; ++m)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) o[g][m][i] = o[g][m][i] * f0 + other[(m * 16 + i) * kWave] * f1;
-      }
+        for (int i = 0; i < 16; ++i) o[m][i] = o[m][i] * f0 + part[(m * 16 + i) * kWave] * f1;
     }
   }
 
-  bool finish = true;
   if (it.pieces > 1) {
     const rsrc_t ru = make_rsrc(reinterpret_cast<char*>(a.part) + static_cast<int64_t>(it.slot) * C::PART,
                                 it.pieces * C::PART);
-    // of this lane: quad i at 1 KiB steps, then (reference, sum) per group
-    const uint32_t at = (wr * (C::QUADS * 16 + NG * 8)) * kWave;
+    // of this lane: quad i at 1 KiB steps, then (reference, sum)
+    const uint32_t at = wr * (C::QUADS * 16 + 8) * kWave;
     auto quad = [&](int i) { return at + i * 16 * kWave + lane * 16; };
-    auto stats = [&](int g) { return at + C::QUADS * 16 * kWave + g * 8 * kWave + lane * 8; };
+    const uint32_t stats = at + C::QUADS * 16 * kWave + lane * 8;
     if (kg == 0) {
       const uint32_t mine = it.piece * C::PART;
 #pragma unroll
-      for (int g = 0; g < NG; ++g) {
-#pragma unroll
-        for (int m = 0; m < NM; ++m)
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            __builtin_amdgcn_raw_buffer_store_b128(
-                __builtin_bit_cast(u32x4, f32x4{o[g][m][4 * i], o[g][m][4 * i + 1], o[g][m][4 * i + 2], o[g][m][4 * i + 3]}),
-                ru, mine + quad((g * NM + m) * 4 + i), 0, kCoherent);
-        __builtin_amdgcn_raw_buffer_store_b64(
-            u32x2{__builtin_bit_cast(uint32_t, ref[g]), __builtin_bit_cast(uint32_t, sum[g])}, ru, mine + stats(g), 0,
-            kCoherent);
+      for (int i = 0; i < C::QUADS; ++i) {
+        const f32x4 x = {o[i / 4][i % 4 * 4], o[i / 4][i % 4 * 4 + 1], o[i / 4][i % 4 * 4 + 2], o[i / 4][i % 4 * 4 + 3]};
+        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, x), ru, mine + quad(i), 0, kCoherent);
       }
+      __builtin_amdgcn_raw_buffer_store_b64(
+          u32x2{__builtin_bit_cast(uint32_t, ref), __builtin_bit_cast(uint32_t, sum)}, ru, mine + stats, 0, kCoherent);
     }
     mem_done();
     __syncthreads();
@@ -479,65 +464,46 @@ __global__ void __launch_bounds__(CTH, NG == 1 ? 2 : 1) attn_chunk_kernel(AttnAr
                static_cast<uint32_t>(it.pieces - 1);
     __syncthreads();
     // the last piece to arrive joins them all, in their order
-    finish = lds[0] != 0;
-    if (finish) {
-      if (threadIdx.x == 0) sync_store(a.arrived + it.unit, 0u);
-      if (kg == 0) {
+    if (lds[0] == 0) return;
+    if (threadIdx.x == 0) sync_store(a.arrived + it.unit, 0u);
+    if (kg == 0) {
+      ref = -INFINITY;
+      sum = 0.f;
 #pragma unroll
-        for (int g = 0; g < NG; ++g) {
-          ref[g] = -INFINITY;
-          sum[g] = 0.f;
+      for (int m = 0; m < NM; ++m) o[m] = f32x16{};
+      for (int c = 0; c < it.pieces; ++c) {
+        float r, t;
+        buf_ld_shared2(ru, c * C::PART + stats, r, t);
+        u32x4 x[C::QUADS];
 #pragma unroll
-          for (int m = 0; m < NM; ++m) o[g][m] = f32x16{};
-        }
-        for (int c = 0; c < it.pieces; ++c) {
-          u32x4 y[NG][NM * 4];
-          float yr[NG], yt[NG];
+        for (int i = 0; i < C::QUADS; ++i)
+          x[i] = __builtin_amdgcn_raw_buffer_load_b128(ru, c * C::PART + quad(i), 0, kCoherent);
+        const float top = fmaxf(ref, r), base = top == -INFINITY ? 0.f : top;
+        const float f0 = __builtin_amdgcn_exp2f(ref - base), f1 = __builtin_amdgcn_exp2f(r - base);
+        ref = top;
+        sum = sum * f0 + t * f1;
 #pragma unroll
-          for (int g = 0; g < NG; ++g) {
-            buf_ld_shared2(ru, c * C::PART + stats(g), yr[g], yt[g]);
+        for (int i = 0; i < C::QUADS; ++i)
 #pragma unroll
-            for (int i = 0; i < NM * 4; ++i)
-              y[g][i] = __builtin_amdgcn_raw_buffer_load_b128(ru, c * C::PART + quad(g * NM * 4 + i), 0, kCoherent);
-          }
-#pragma unroll
-          for (int g = 0; g < NG; ++g) {
-            const float top = fmaxf(ref[g], yr[g]), base = top == -INFINITY ? 0.f : top;
-            const float f0 = __builtin_amdgcn_exp2f(ref[g] - base), f1 = __builtin_amdgcn_exp2f(yr[g] - base);
-            ref[g] = top;
-            sum[g] = sum[g] * f0 + yt[g] * f1;
-#pragma unroll
-            for (int i = 0; i < NM * 4; ++i)
-#pragma unroll
-              for (int e = 0; e < 4; ++e)
-                o[g][i / 4][i % 4 * 4 + e] =
-                    o[g][i / 4][i % 4 * 4 + e] * f0 + f1 * __builtin_bit_cast(f32x4, y[g][i])[e];
-          }
-        }
+          for (int e = 0; e < 4; ++e)
+            o[i / 4][i % 4 * 4 + e] = o[i / 4][i % 4 * 4 + e] * f0 + f1 * __builtin_bit_cast(f32x4, x[i])[e];
       }
     }
   }
-  if (finish && kg == 0) {
-    const float vs = F8 && a.p.v_scale ? a.p.v_scale[it.head] : 1.f;
+  if (kg != 0 || !there) return;
+  const float vs = F8 && a.p.v_scale ? a.p.v_scale[it.head] : 1.f;
+  const float inv = sum == 0.f ? 0.f : vs / sum;
+  uint16_t* op = a.out + (q.b + tok) * a.ld_out + static_cast<int64_t>(head) * D + 4 * hf;
+  // accumulator i of tile m is element 32 m + 8 (i / 4) + 4 hf + i % 4
 #pragma unroll
-    for (int g = 0; g < NG; ++g) {
-      if (!there[g]) continue;
-      const int tok = row[g] / a.group, hd = it.head * a.group + row[g] - tok * a.group;
-      const float inv = sum[g] == 0.f ? 0.f : vs / sum[g];
-      uint16_t* op = a.out + (q.b + tok) * a.ld_out + static_cast<int64_t>(hd) * D + 4 * hf;
-      // accumulator i of tile m is element 32 m + 8 (i / 4) + 4 hf + i % 4
+  for (int m = 0; m < NM; ++m)
 #pragma unroll
-      for (int m = 0; m < NM; ++m)
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          *reinterpret_cast<u32x2*>(op + 32 * m + 8 * i) =
-              u32x2{T::pack2(o[g][m][4 * i] * inv, o[g][m][4 * i + 1] * inv),
-                    T::pack2(o[g][m][4 * i + 2] * inv, o[g][m][4 * i + 3] * inv)};
-      if (a.lse && hf == 0)
-        a.lse[static_cast<int64_t>(q.b + tok) * a.n_q + hd] =
-            sum[g] == 0.f ? -INFINITY : (ref[g] + __builtin_amdgcn_logf(sum[g])) * 0.6931471805599453f;
-    }
-  }
+    for (int i = 0; i < 4; ++i)
+      *reinterpret_cast<u32x2*>(op + 32 * m + 8 * i) = u32x2{T::pack2(o[m][4 * i] * inv, o[m][4 * i + 1] * inv),
+                                                             T::pack2(o[m][4 * i + 2] * inv, o[m][4 * i + 3] * inv)};
+  if (a.lse && hf == 0)
+    a.lse[static_cast<int64_t>(q.b + tok) * a.n_q + head] =
+        sum == 0.f ? -INFINITY : (ref + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f;
 }
 
 hipError_t launch_chunk(const AttnArgs& a, int type, bool f8, int head_dim, int tile, hipStream_t s) {
@@ -548,13 +514,13 @@ hipError_t launch_chunk(const AttnArgs& a, int type, bool f8, int head_dim, int 
     constexpr int D = decltype(DD)::value;
     constexpr bool f = decltype(F)::value, b = decltype(B)::value;
     if (tile == 64) {
-      rows = Chunk<D, 1, 2>::ROWS;
-      shared = std::max<int>(Chunk<D, 1, 2>::LDS, Chunk<D, 1, 2>::RGW * (D / 2 + 2) * kWave * 4);
-      return attn_chunk_kernel<T, f, D, b, 1, 2>;
+      rows = Chunk<D, 2>::ROWS;
+      shared = std::max<int>(Chunk<D, 2>::LDS, Chunk<D, 2>::RGW * (D / 2 + 2) * kWave * 4);
+      return attn_chunk_kernel<T, f, D, b, 2>;
     }
-    rows = Chunk<D, 1, 1>::ROWS;
-    shared = Chunk<D, 1, 1>::LDS;
-    return attn_chunk_kernel<T, f, D, b, 1, 1>;
+    rows = Chunk<D, 1>::ROWS;
+    shared = Chunk<D, 1>::LDS;
+    return attn_chunk_kernel<T, f, D, b, 1>;
   };
   auto pick3 = [&](auto X, auto F, auto B) {
     return head_dim == 128 ? pick(X, F, B, std::integral_constant<int, 128>{})
