@@ -61,6 +61,31 @@ __device__ __forceinline__ void dma_lanes(uint32_t to, const char* p) {
 
 __device__ __forceinline__ int swap_bits23(int r) { return (r & ~12) | ((r & 4) << 1) | ((r & 8) >> 1); }
 
+// A block's scores to weights in eight steps, to stand between products: step i forms the
+// exponentials of numbers 2 i and 2 i + 1 and packs and adds up those of the step before.
+template <class T>
+struct Weights {
+  const f32x16& s;
+  const float sc, base;
+  float e0, e1;
+  __device__ __forceinline__ Weights(const f32x16& s, float sc, float base) : s(s), sc(sc), base(base) {}
+  __device__ __forceinline__ void step(int i, u32x4 (&pf)[2], float& sum, float& top) {
+    float x0 = fmaf(s[2 * i], sc, -base), x1 = fmaf(s[2 * i + 1], sc, -base);
+    top = fmaxf(top, fmaxf(s[2 * i], s[2 * i + 1]));
+    if (i > 0) put(i - 1, pf, sum);
+    e0 = __builtin_amdgcn_exp2f(x0);
+    e1 = __builtin_amdgcn_exp2f(x1);
+    asm volatile("" : "+v"(e0), "+v"(e1), "+v"(top), "+v"(sum));  // (here, not where they are used)
+  }
+  __device__ __forceinline__ void end(u32x4 (&pf)[2], float& sum) { put(7, pf, sum); }
+
+ private:
+  __device__ __forceinline__ void put(int i, u32x4 (&pf)[2], float& sum) {
+    sum += e0 + e1;
+    pf[i / 4][i % 4] = T::pack2(e0, e1);
+  }
+};
+
 // KG groups of waves share the rows and take every KG-th block of 32 keys.
 template <int D, int KG>
 struct Chunk {
@@ -250,16 +275,26 @@ __global__ void __launch_bounds__(CTH, 2) attn_chunk_kernel(AttnArgs a) {
   const int kr = swap_bits23(ql);
   // A lane's parts of a block at S: chunk c of its key, and element 32 m + l % 32 of keys
   // 16 b + 8 hf .. + 7.
-  auto kfrag = [&](const char* S, int c) {
-    return *reinterpret_cast<const u32x4*>(S + (kr * D * 2 + ((2 * c + hf) ^ (kr % CPR)) * 16));
-  };
+  // The swizzles are exclusive ors, so the chunks of a lane's key differ from its first one's
+  // address in the bits of 32 c, and those of its values in the bits of 64 m (and, where h moves
+  // their row by 4, of 128 h): a register for each of these, the rest in the instructions.
+  const uint32_t kbase = kr * D * 2 + (hf ^ (kr % CPR)) * 16;
+  const uint32_t vbase = vkey * D * 2 + (vdim ^ (2 * (vkey % (CPR / 2)))) * 16 + (jl % 2) * 8;
+  uint32_t kat[NK], vat[NM];
+#pragma unroll
+  for (int c = 0; c < NK; ++c) kat[c] = kbase ^ (32 * c);
+#pragma unroll
+  for (int m = 0; m < NM; ++m) vat[m] = vbase ^ (64 * m);
+#pragma unroll
+  for (int c = 0; c < NK; ++c) asm volatile("" : "+v"(kat[c]));
+#pragma unroll
+  for (int m = 0; m < NM; ++m) asm volatile("" : "+v"(vat[m]));
+  auto kfrag = [&](const char* S, int c) { return *reinterpret_cast<const u32x4*>(S + kat[c]); };
   auto vfrag = [&](const char* S, int m, int b) {
     u32x4 f;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const int r = vkey + 4 * h;
-      const u32x2 x = lds_read_tr(S + KV + 16 * b * D * 2 +
-                                  (r * D * 2 + ((4 * m + vdim) ^ (2 * (r % (CPR / 2)))) * 16 + (jl % 2) * 8));
+      const u32x2 x = lds_read_tr(S + KV + (16 * b + 4 * h) * D * 2 + vat[D == 128 ? m ^ (2 * h) : m]);
       f[2 * h] = x[0];
       f[2 * h + 1] = x[1];
     }
@@ -285,7 +320,7 @@ __global__ void __launch_bounds__(CTH, 2) attn_chunk_kernel(AttnArgs a) {
       for (int i = 0; i < 16; ++i) o[m][i] *= alpha;
   };
   // scores to weights, the second product's operand, and their sum
-  auto weigh = [&](const f32x16& s, u32x4 (&pf)[2]) {
+  auto weigh = [&](const f32x16& s, u32x4 (&pf)[2], float& sum) {
     const float base = ref == -INFINITY ? 0.f : ref;
 #pragma unroll
     for (int w = 0; w < 8; ++w) {
@@ -295,58 +330,74 @@ __global__ void __launch_bounds__(CTH, 2) attn_chunk_kernel(AttnArgs a) {
       pf[w / 4][w % 4] = T::pack2(pa, pb);
     }
   };
-  // A block that some rows of the wave do not see whole, from key p0 on; gone: its keys on
-  // bad pages.
-  auto partly = [&](const char* S, int p0, uint32_t gone) {
+  // Bits of keys lo .. hi - 1 of the block of 32 from key p0 on.
+  auto span = [](int p0, int lo, int hi) {
+    const int l = min(max(lo - p0, 0), 32), h = min(max(hi - p0, 0), 32);
+    return static_cast<uint32_t>(((uint64_t(1) << h) - 1) & ~((uint64_t(1) << l) - 1));
+  };
+  // The lane's 16 of a block's 32 bits: accumulator 8 b + e is key 16 b + 8 hf + e.
+  auto own16 = [&](uint32_t w) { return (w >> (8 * hf) & 0xFFu) | (w >> (8 + 8 * hf) & 0xFF00u); };
+  // One block by itself, from key p0 on, with a new reference: one that some rows of the wave
+  // do not see whole, or whose scores ask for it; gone: its keys on bad pages.
+  auto single = [&](const char* S, int p0, uint32_t gone) {
     f32x16 s = f32x16{};
 #pragma unroll
     for (int c = 0; c < NK; ++c) s = T::mfma32(kfrag(S, c), qf[c], s);
-    // the lane's keys: accumulator 8 b + e is key p0 + 16 b + 8 hf + e
-    auto key = [&](int i) { return p0 + 16 * (i / 8) + 8 * hf + i % 8; };
-    const uint32_t bad = (gone >> (8 * hf) & 0xFFu) | (gone >> (8 + 8 * hf) & 0xFF00u);
-    bool seen = false;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const bool in = key(i) >= klo && key(i) < khi;
-      if (!in || (bad >> i & 1)) s[i] = -INFINITY;
-      seen |= in && there && (bad >> i & 1);
-    }
-    if (__builtin_amdgcn_ballot_w64(seen) != 0 && a.p.status) sync_or(a.p.status, VT_PAGED_BAD_PAGE);
     u32x4 pf[2];
+    const uint32_t mine = span(p0, klo, khi), sees = own16(mine & ~gone);
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+      if (!(sees >> i & 1)) s[i] = -INFINITY;
+    if (__builtin_amdgcn_ballot_w64(there && (mine & gone)) != 0 && a.p.status)
+      sync_or(a.p.status, VT_PAGED_BAD_PAGE);
     refer(largest(s));
-    weigh(s, pf);
+    weigh(s, pf, sum);
     // values that no row of the wave sees stay out of the product even if they are
-    // infinite; where some rows see an infinite or NaN value and others do not, each row
-    // gets a product of its own
+    // infinite
+    const uint32_t used = own16(span(p0, any_lo, any_hi) & ~gone);
+    auto seen = [&](int m, int b, uint32_t keys) {  // a fragment's values of these of the lane's keys
+      u32x4 z = vfrag(S, m, b);
+#pragma unroll
+      for (int w = 0; w < 4; ++w)
+        z[w] &= (keys >> (8 * b + 2 * w) & 1 ? 0xFFFFu : 0u) | (keys >> (8 * b + 2 * w + 1) & 1 ? 0xFFFF0000u : 0u);
+      return z;
+    };
+    uint32_t odd = 0;  // a zero half among the exponents' complements: an infinity or a NaN
 #pragma unroll
     for (int m = 0; m < NM; ++m)
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
-        u32x4 vf = vfrag(S, m, b);
-        bool odd = false;
+        const u32x4 z = seen(m, b, used);
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-          if (key(8 * b + e) < any_lo || key(8 * b + e) >= any_hi || (bad >> (8 * b + e) & 1))
-            vf[e / 2] &= e % 2 ? 0x0000FFFFu : 0xFFFF0000u;
-#pragma unroll
-        for (int w = 0; w < 4; ++w) odd |= odd2<T>(vf[w]);
-        if (__builtin_amdgcn_ballot_w64(odd) == 0) {
-          o[m] = T::mfma32(vf, pf[b], o[m]);
-          continue;
+        for (int w = 0; w < 4; ++w) {
+          const uint32_t c = ~z[w] & T::kExp;
+          odd |= (c - 0x00010001u) & ~c & 0x80008000u;
         }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    if (__builtin_amdgcn_ballot_w64(odd != 0) != 0) {
+      // where some rows see an infinite or NaN value and others do not, each row gets a
+      // product of its own, with what it does not see set to zero
+#pragma unroll
+      for (int m = 0; m < NM; ++m) {
         f32x16 keep = o[m];
 #pragma unroll 1
         for (int c = 0; c < 32; ++c) {
-          const int lo_c = __builtin_amdgcn_readlane(klo, c), hi_c = __builtin_amdgcn_readlane(khi, c);
-          u32x4 z = vf;
+          const uint32_t row =
+              own16(span(p0, __builtin_amdgcn_readlane(klo, c), __builtin_amdgcn_readlane(khi, c)) & ~gone);
+          f32x16 r = o[m];
 #pragma unroll
-          for (int e = 0; e < 8; ++e)
-            if (key(8 * b + e) < lo_c || key(8 * b + e) >= hi_c) z[e / 2] &= e % 2 ? 0x0000FFFFu : 0xFFFF0000u;
-          const f32x16 r = T::mfma32(z, pf[b], o[m]);
+          for (int b = 0; b < 2; ++b) r = T::mfma32(seen(m, b, row), pf[b], r);
           if (ql == c) keep = r;
         }
         o[m] = keep;
       }
+      return;
+    }
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int m = 0; m < NM; ++m) o[m] = T::mfma32(seen(m, b, used), pf[b], o[m]);
   };
 
   if (stages > 0) {
@@ -380,36 +431,104 @@ __global__ void __launch_bounds__(CTH, 2) attn_chunk_kernel(AttnArgs a) {
     auto place = [&](int t) { return smem + (t / BPS) % C::NST * C::STAGE + sub_of(t) * 32 * D * 2; };
     int t = 0;
     while (t < blocks) {
-      for (; t < blocks; ++t) {
-        const int k0 = first_key(t);
-        if (k0 < full_lo || k0 + 32 > full_hi) break;
-        begin(t / BPS);
-        if (__builtin_amdgcn_readfirstlane(absent[t / BPS % C::NST][sub_of(t)]) != 0) break;
-        const char* B = place(t);
-        // all fragments are on their way before the first is used: V's arrive behind the scores
-        u32x4 kf[NK], vf[NM][2], pf[2];
+      // A stage's two blocks A and B overlap: B's scores with A's weights, A's product with B's
+      // weights. Weights against a reference that turns out too low are dropped before
+      // they are used.
+      if constexpr (KG == 1) {
+        for (; t + 2 <= blocks; t += 2) {
+          const int k0 = (b0 + t / 2) * KS;
+          if (t % 2 != 0 || k0 < full_lo || k0 + KS > full_hi) break;
+          begin(t / 2);
+          const int gone = absent[t / 2 % C::NST][0] | absent[t / 2 % C::NST][1];
+          if (__builtin_amdgcn_readfirstlane(gone) != 0) break;
+          const char* A = place(t);
+          const char* B = A + 32 * D * 2;
+          u32x4 kf[NK], vf[NM][2], pa[2], pb[2];
+          f32x16 sa = f32x16{}, sb = f32x16{};
+          const float base = ref == -INFINITY ? 0.f : ref;
 #pragma unroll
-        for (int c = 0; c < NK; ++c) kf[c] = kfrag(B, c);
+          for (int c = 0; c < NK; ++c) kf[c] = kfrag(A, c);
 #pragma unroll
-        for (int m = 0; m < NM; ++m)
+          for (int c = 0; c < NK; ++c) {
+            sa = T::mfma32(kf[c], qf[c], sa);
+            kf[c] = kfrag(B, c);
+            asm volatile("" : "+v"(sa));
+          }
 #pragma unroll
-          for (int b = 0; b < 2; ++b) vf[m][b] = vfrag(B, m, b);
-        __builtin_amdgcn_sched_barrier(0);
-        f32x16 s = f32x16{};
+          for (int m = 0; m < NM; ++m)
 #pragma unroll
-        for (int c = 0; c < NK; ++c) s = T::mfma32(kf[c], qf[c], s);
-        if (__builtin_amdgcn_ballot_w64(largest(s) > ref + 8.f) != 0) break;
-        weigh(s, pf);
+            for (int b = 0; b < 2; ++b) vf[m][b] = vfrag(A, m, b);
+          float suma = 0.f, sumb = 0.f, topa = -INFINITY, topb = -INFINITY;
+          Weights<T> wa(sa, sc, base), wb(sb, sc, base);
 #pragma unroll
-        for (int m = 0; m < NM; ++m)
+          for (int i = 0; i < 8; ++i) {
 #pragma unroll
-          for (int b = 0; b < 2; ++b) o[m] = T::mfma32(vf[m][b], pf[b], o[m]);
+            for (int c = i * NK / 8; c < (i + 1) * NK / 8; ++c) sb = T::mfma32(kf[c], qf[c], sb);
+            wa.step(i, pa, suma, topa);
+            asm volatile("" : "+v"(sb));
+            __builtin_amdgcn_sched_barrier(0);
+          }
+          wa.end(pa, suma);
+          const bool raise_a = __builtin_amdgcn_ballot_w64(topa * sc > ref + 8.f) != 0;
+          asm volatile("" : "+v"(pa[0]), "+v"(pa[1]), "+v"(suma));
+          if (raise_a) break;
+          sum += suma;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+#pragma unroll
+            for (int j = i * NM / 4; j < (i + 1) * NM / 4; ++j) {
+              const int m = j % NM, b = j / NM;
+              o[m] = T::mfma32(vf[m][b], pa[b], o[m]);
+              vf[m][b] = vfrag(B, m, b);
+            }
+            wb.step(i, pb, sumb, topb);
+            __builtin_amdgcn_sched_barrier(0);
+          }
+          wb.end(pb, sumb);
+          const bool raise_b = __builtin_amdgcn_ballot_w64(topb * sc > ref + 8.f) != 0;
+          asm volatile("" : "+v"(pb[0]), "+v"(pb[1]), "+v"(sumb));
+          if (raise_b) {
+            ++t;  // A is done
+            break;
+          }
+          sum += sumb;
+#pragma unroll
+          for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int m = 0; m < NM; ++m) o[m] = T::mfma32(vf[m][b], pb[b], o[m]);
+        }
+      } else {
+        for (; t < blocks; ++t) {
+          const int k0 = first_key(t);
+          if (k0 < full_lo || k0 + 32 > full_hi) break;
+          begin(t / BPS);
+          if (__builtin_amdgcn_readfirstlane(absent[t / BPS % C::NST][sub_of(t)]) != 0) break;
+          const char* B = place(t);
+          // all fragments are on their way before the first is used: V's arrive behind the scores
+          u32x4 kf[NK], vf[NM][2], pf[2];
+#pragma unroll
+          for (int c = 0; c < NK; ++c) kf[c] = kfrag(B, c);
+#pragma unroll
+          for (int m = 0; m < NM; ++m)
+#pragma unroll
+            for (int b = 0; b < 2; ++b) vf[m][b] = vfrag(B, m, b);
+          __builtin_amdgcn_sched_barrier(0);
+          f32x16 s = f32x16{};
+#pragma unroll
+          for (int c = 0; c < NK; ++c) s = T::mfma32(kf[c], qf[c], s);
+          if (__builtin_amdgcn_ballot_w64(largest(s) > ref + 8.f) != 0) break;
+          weigh(s, pf, sum);
+#pragma unroll
+          for (int m = 0; m < NM; ++m)
+#pragma unroll
+            for (int b = 0; b < 2; ++b) o[m] = T::mfma32(vf[m][b], pf[b], o[m]);
+        }
       }
       if (t >= blocks) break;
       begin(t / BPS);
       const int k0 = first_key(t);
-      if (k0 < any_hi && k0 + 32 > any_lo)  // some row of this wave sees some of it
-        partly(place(t), k0, __builtin_amdgcn_readfirstlane(absent[t / BPS % C::NST][sub_of(t)]));
+      const uint32_t gone = __builtin_amdgcn_readfirstlane(absent[t / BPS % C::NST][sub_of(t)]);
+      if (k0 < any_hi && k0 + 32 > any_lo) single(place(t), k0, gone);  // some row of the wave sees some of it
       ++t;
     }
   }
