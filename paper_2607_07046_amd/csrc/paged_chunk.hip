@@ -92,8 +92,7 @@ struct Chunk {
   static constexpr int RGW = CW / KG;           // waves side by side over the rows
   static constexpr int ROWS = RGW * 32;
   static constexpr int STAGE = KS * D * 2 * 2;  // bytes of a stage: K, then V
-  static constexpr int NST = 2;
-  static constexpr int LDS = STAGE * NST;
+  static constexpr int LDS = 2 * STAGE;
   // a partial result of a wave: [register quad][lane][4], then a reference and a sum per lane
   static constexpr int QUADS = D / 8;
   static constexpr uint32_t PART = RGW * kWave * (QUADS * 16 + 8);
@@ -107,7 +106,7 @@ __global__ void __launch_bounds__(CTH, 2) attn_chunk_kernel(AttnArgs a) {
   constexpr int KV = KS * D * 2;  // bytes of a stage's K
   extern __shared__ __attribute__((aligned(16))) char smem[];
   __shared__ int lds[32];
-  __shared__ uint32_t absent[C::NST][KS / 32];  // of a stage's keys: bit i of word b, key 32 b + i is on a bad page
+  __shared__ uint32_t absent[2][KS / 32];  // of a stage's keys: bit i of word b, key 32 b + i is on a bad page
   const int lane = threadIdx.x % kWave, ql = lane % 32, hf = lane / 32;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int wr = wave % C::RGW, kg = wave / C::RGW;
@@ -170,86 +169,101 @@ __global__ void __launch_bounds__(CTH, 2) attn_chunk_kernel(AttnArgs a) {
   for (int m = 0; m < NM; ++m) o[m] = f32x16{};
 
   // ---- stages into LDS -------------------------------------------------------
-  // A stage's page numbers are looked up a stage ahead of its loads. IDS: those a
-  // lane needs, of loads u of its wave.
-  constexpr int LPW = F8 ? D / 64 : D / 32;          // loads of K (and of V) per wave: 16 rows, or (8-bit) 8 or 16 of them
-  constexpr int RPL = F8 ? 1024 / D : 512 / D;       // rows of a load
-  constexpr int LPR = kWave / RPL;                   // lanes of a row
+  // A wave loads 16 rows of K and of V, LPW loads of RPL rows each: 16 rows together, or (8-bit,
+  // D 128) two times 8. Their page numbers are looked up a stage ahead. With pages of 16
+  // and more (BIG) rows that are loaded together are on one page: one address for the wave,
+  // and offsets of its lanes that are the same in every stage.
+  constexpr int LPW = F8 ? D / 64 : D / 32, RPL = F8 ? 1024 / D : 512 / D;
+  constexpr int LPR = kWave / RPL;                       // lanes of a row
+  constexpr int UPG = F8 ? 1 : LPW, GR = LPW / UPG;      // loads of a group of rows, groups
   const int lrow = lane / LPR, lcol = lane % LPR;
-  // rows of load u of this wave in the stage
-  auto first_row = [&](int u) { return F8 ? u * (CW * RPL) + wave * RPL : wave * 16 + u * RPL; };
-  int ids[BIG ? (F8 ? LPW : 1) : LPW];
+  auto first_row = [&](int g) { return F8 ? g * (CW * RPL) + wave * RPL : wave * 16; };
+  // byte offset of the lane's chunk of row u * RPL + lrow of a group, as LDS takes them: in the order
+  // of the places, swizzled
+  auto chunk_k = [&](int u) { return F8 ? lcol * 16 : (lcol ^ ((u * RPL + lrow) % CPR)) * 16; };
+  auto chunk_v = [&](int u) { return F8 ? lcol * 16 : (lcol ^ (2 * ((u * RPL + lrow) % (CPR / 2)))) * 16; };
+  constexpr bool AHEAD = F8;  // offsets kept from stage to stage: one register; for 16 bits they are eight and not there
+  uint32_t koff[UPG], voff[UPG];
+#pragma unroll
+  for (int u = 0; u < UPG; ++u) {
+    koff[u] = (u * RPL + lrow) * slot + chunk_k(u);
+    voff[u] = (u * RPL + lrow) * slot + chunk_v(u);
+  }
+  int ids[BIG ? GR : LPW];
   u32x4 kreg[F8 ? LPW : 1], vreg[F8 ? LPW : 1];
   auto look = [&](int st) {
     const int p0 = (b0 + min(st, stages - 1)) * KS;
     if constexpr (BIG) {
 #pragma unroll
-      for (int u = 0; u < (F8 ? LPW : 1); ++u) ids[u] = tab[min(p0 + first_row(u), last) >> a.p.shift];
+      for (int g = 0; g < GR; ++g) ids[g] = tab[min(p0 + first_row(g), last) >> a.p.shift];
     } else {
 #pragma unroll
-      for (int u = 0; u < LPW; ++u) ids[u] = tabv[min(p0 + first_row(u) + lrow, last) >> a.p.shift];
+      for (int u = 0; u < LPW; ++u)
+        ids[u] = tabv[min(p0 + first_row(u / UPG) + u % UPG * RPL + lrow, last) >> a.p.shift];
     }
   };
   auto fetch = [&](int st) {
-    const int p0 = (b0 + min(st, stages - 1)) * KS;
-    const uint32_t to = lbase + (st % C::NST) * C::STAGE;
-    uint32_t gone = 0;  // bad pages among the rows of the wave's loads so far
+    const int p0 = (b0 + st) * KS, par = st & 1;
 #pragma unroll
-    for (int u = 0; u < LPW; ++u) {
-      const int id = ids[BIG ? (F8 ? u : 0) : u];
-      const bool ok = id >= 0 && id < a.p.n_pages;
-      const int64_t page = static_cast<int64_t>(ok ? id : 0) * a.p.page;
-      if constexpr (BIG) {
-        if (!ok) gone |= ((1u << RPL) - 1) << (F8 ? 0 : u * RPL);
-      } else {
-        const uint64_t m = __builtin_amdgcn_ballot_w64(!ok);
-        if (m)
-#pragma unroll
-          for (int i = 0; i < RPL; ++i) gone |= static_cast<uint32_t>(m >> (i * LPR) & 1) << (F8 ? i : u * RPL + i);
-      }
-      if (F8 || u == LPW - 1) {
-        char* flag = reinterpret_cast<char*>(absent[st % C::NST]) + (F8 ? first_row(u) : wave * 16) / 8;
-        // (every lane stores it: a branch that lanes take apart would cost the stages' loop its plain flow)
-        if (F8 && RPL == 8) *reinterpret_cast<uint8_t*>(flag) = static_cast<uint8_t>(gone);
-        else *reinterpret_cast<uint16_t*>(flag) = static_cast<uint16_t>(gone);
-        gone = 0;
-      }
-      const int r0 = first_row(u), r = r0 + lrow;
-      const char *kp, *vp;  // of the lane's row
-      uint32_t off = 0;
-      if constexpr (BIG) {
-        const int key = min(p0 + r0, last);
-        const int64_t at = page + static_cast<int64_t>(key & a.p.mask) * a.p.slot;
-        kp = kb + at;
-        vp = vb + at;
-        off = static_cast<uint32_t>(min(lrow, last - key)) * slot;  // rows past the last position read that one again
-      } else {
-        const int64_t at = page + static_cast<int64_t>(min(p0 + r, last) & a.p.mask) * a.p.slot;
-        kp = kb + at;
-        vp = vb + at;
-      }
-      if constexpr (F8) {
-        kreg[u] = *reinterpret_cast<const u32x4*>(kp + off + lcol * 16);
-        vreg[u] = *reinterpret_cast<const u32x4*>(vp + off + lcol * 16);
-      } else {
-        const uint32_t kc = (lcol ^ (r % CPR)) * 16, vc = (lcol ^ (2 * (r % (CPR / 2)))) * 16;
-        const uint32_t tk = __builtin_amdgcn_readfirstlane(to + r0 * D * 2);
-        if constexpr (BIG) {
-          dma_rows(tk, kp, off + kc);
-          dma_rows(tk + KV, vp, off + vc);
+    for (int g = 0; g < GR; ++g) {
+      const int r0 = first_row(g);
+      const uint32_t to = __builtin_amdgcn_readfirstlane(lbase + par * C::STAGE + r0 * D * 2);
+      uint32_t gone = 0;  // the group's rows on bad pages
+      // one load of K and V: from lane addresses, or a wave's and a lane's offsets
+      auto get = [&](int u, const char* kp, const char* vp, uint32_t ko, uint32_t vo) {
+        if constexpr (F8) {
+          kreg[g] = *reinterpret_cast<const u32x4*>(kp + ko);
+          vreg[g] = *reinterpret_cast<const u32x4*>(vp + vo);
+        } else if constexpr (BIG) {
+          dma_rows(to + u * 1024, kp, ko);
+          dma_rows(to + u * 1024 + KV, vp, vo);
         } else {
-          dma_lanes(tk, kp + kc);
-          dma_lanes(tk + KV, vp + vc);
+          dma_lanes(to + u * 1024, kp + ko);
+          dma_lanes(to + u * 1024 + KV, vp + vo);
+        }
+      };
+      if constexpr (BIG) {
+        const bool ok = static_cast<uint32_t>(ids[g]) < static_cast<uint32_t>(a.p.n_pages);
+        gone = ok ? 0u : (1u << (UPG * RPL)) - 1;
+        const int key = min(p0 + r0, last);
+        const uint64_t at = static_cast<uint64_t>(ok ? static_cast<uint32_t>(ids[g]) : 0u) * static_cast<uint64_t>(a.p.page) +
+                            static_cast<uint64_t>(static_cast<uint32_t>(key & a.p.mask)) * slot;
+        if (AHEAD && __builtin_expect(p0 + r0 + UPG * RPL - 1 <= last, 1)) {
+#pragma unroll
+          for (int u = 0; u < UPG; ++u) get(u, kb + at, vb + at, koff[u], voff[u]);
+        } else {  // rows past the last position read that one again
+#pragma unroll
+          for (int u = 0; u < UPG; ++u) {
+            const uint32_t row = static_cast<uint32_t>(min(u * RPL + lrow, last - key)) * slot;
+            get(u, kb + at, vb + at, row + chunk_k(u), row + chunk_v(u));
+          }
+        }
+      } else {
+#pragma unroll
+        for (int u = 0; u < UPG; ++u) {
+          const int id = ids[g * UPG + u];
+          const bool ok = id >= 0 && id < a.p.n_pages;
+          const uint64_t m = __builtin_amdgcn_ballot_w64(!ok);
+          if (m)
+#pragma unroll
+            for (int i = 0; i < RPL; ++i) gone |= static_cast<uint32_t>(m >> (i * LPR) & 1) << (u * RPL + i);
+          const int64_t at = static_cast<int64_t>(ok ? id : 0) * a.p.page +
+                             static_cast<int64_t>(min(p0 + r0 + u * RPL + lrow, last) & a.p.mask) * a.p.slot;
+          get(u, kb + at, vb + at, chunk_k(u), chunk_v(u));
         }
       }
+      // (every lane stores it: a branch that lanes take apart would cost the stages' loop its plain flow)
+      char* flag = reinterpret_cast<char*>(absent[par]) + r0 / 8;
+      if (UPG * RPL == 8) *reinterpret_cast<uint8_t*>(flag) = static_cast<uint8_t>(gone);
+      else *reinterpret_cast<uint16_t*>(flag) = static_cast<uint16_t>(gone);
     }
   };
   // 8-bit: what fetch loaded, widened into its stage
   auto widen = [&](int st) {
     if constexpr (F8) {
-      char* S = smem + (st % C::NST) * C::STAGE;
+      char* S = smem + (st & 1) * C::STAGE;
 #pragma unroll
-      for (int u = 0; u < LPW; ++u) {
+      for (int u = 0; u < GR; ++u) {
         const int r = first_row(u) + lrow;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
@@ -426,9 +440,10 @@ __global__ void __launch_bounds__(CTH, 2) attn_chunk_kernel(AttnArgs a) {
     // moved between registers at every block.
     constexpr int BPS = 2 / KG;
     const int blocks = stages * BPS;
-    auto sub_of = [&](int t) { return KG == 2 ? kg : t % 2; };
-    auto first_key = [&](int t) { return (b0 + t / BPS) * KS + sub_of(t) * 32; };
-    auto place = [&](int t) { return smem + (t / BPS) % C::NST * C::STAGE + sub_of(t) * 32 * D * 2; };
+    auto stage_of = [&](int t) { return KG == 2 ? t : t >> 1; };
+    auto sub_of = [&](int t) { return KG == 2 ? kg : t & 1; };
+    auto first_key = [&](int t) { return (b0 + stage_of(t)) * KS + sub_of(t) * 32; };
+    auto place = [&](int t) { return smem + (stage_of(t) & 1) * C::STAGE + sub_of(t) * 32 * D * 2; };
     int t = 0;
     while (t < blocks) {
       // A stage's two blocks A and B overlap: B's scores with A's weights, A's product with B's
@@ -436,10 +451,10 @@ __global__ void __launch_bounds__(CTH, 2) attn_chunk_kernel(AttnArgs a) {
       // they are used.
       if constexpr (KG == 1) {
         for (; t + 2 <= blocks; t += 2) {
-          const int k0 = (b0 + t / 2) * KS;
-          if (t % 2 != 0 || k0 < full_lo || k0 + KS > full_hi) break;
-          begin(t / 2);
-          const int gone = absent[t / 2 % C::NST][0] | absent[t / 2 % C::NST][1];
+          const int k0 = (b0 + (t >> 1)) * KS;
+          if ((t & 1) != 0 || k0 < full_lo || k0 + KS > full_hi) break;
+          begin(t >> 1);
+          const int gone = absent[t >> 1 & 1][0] | absent[t >> 1 & 1][1];
           if (__builtin_amdgcn_readfirstlane(gone) != 0) break;
           const char* A = place(t);
           const char* B = A + 32 * D * 2;
@@ -501,8 +516,8 @@ __global__ void __launch_bounds__(CTH, 2) attn_chunk_kernel(AttnArgs a) {
         for (; t < blocks; ++t) {
           const int k0 = first_key(t);
           if (k0 < full_lo || k0 + 32 > full_hi) break;
-          begin(t / BPS);
-          if (__builtin_amdgcn_readfirstlane(absent[t / BPS % C::NST][sub_of(t)]) != 0) break;
+          begin(stage_of(t));
+          if (__builtin_amdgcn_readfirstlane(absent[stage_of(t) & 1][sub_of(t)]) != 0) break;
           const char* B = place(t);
           // all fragments are on their way before the first is used: V's arrive behind the scores
           u32x4 kf[NK], vf[NM][2], pf[2];
@@ -525,9 +540,9 @@ __global__ void __launch_bounds__(CTH, 2) attn_chunk_kernel(AttnArgs a) {
         }
       }
       if (t >= blocks) break;
-      begin(t / BPS);
+      begin(stage_of(t));
       const int k0 = first_key(t);
-      const uint32_t gone = __builtin_amdgcn_readfirstlane(absent[t / BPS % C::NST][sub_of(t)]);
+      const uint32_t gone = __builtin_amdgcn_readfirstlane(absent[stage_of(t) & 1][sub_of(t)]);
       if (k0 < any_hi && k0 + 32 > any_lo) single(place(t), k0, gone);  // some row of the wave sees some of it
       ++t;
     }
