@@ -211,9 +211,9 @@ struct Plan {
   int32_t total;   // items in all
   Seq mine;        // this thread's sequence, if it has one only
 
-  // The pieces of a unit are joined by one workgroup, in time that grows with their number:
-  // for tiles of 16 rows a cap that its LDS sets; for the larger ones, whose partial results
-  // are as large as what a stage loads, as many pieces as a piece has blocks.
+  // The pieces of a unit are joined by one workgroup, in time that grows with their number.
+  // A 16-row tile's partial results are small: 128 of them come in a few round trips. Those of
+  // the larger tiles are as large as what two stages load: as many pieces as a piece has blocks.
   __device__ __forceinline__ int pieces(int blocks) const {
     const int cap = ROWS == 16 ? 128 : max(1, static_cast<int>(sqrtf(static_cast<float>(blocks))));
     return min(cap, max(1, (blocks + most - 1) / most));

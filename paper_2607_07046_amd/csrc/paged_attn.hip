@@ -93,9 +93,8 @@ __global__ void __launch_bounds__(RT, 2) attn_rows_kernel(AttnArgs a) {
   constexpr int MLD = D + 4;               // a row of the merge buffer
   __shared__ __attribute__((aligned(16))) float merge[RW][ROWS * MLD];
   __shared__ float merge_ref[RW][ROWS], merge_sum[RW][ROWS];
-  __shared__ float part_top[ROWS][ROWS], part_sum[ROWS][ROWS];
   __shared__ int lds[32];
-  static_assert(kItemWords <= 32 && 2 * 128 * ROWS <= RW * ROWS * MLD, "");  // 128: the most pieces of a unit
+  static_assert(kItemWords <= 32 && 10 * RT <= RW * ROWS * MLD, "");
   const int lane = threadIdx.x % kWave, n = lane % 16, g = lane / 16;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   if (blockIdx.x == 0 && a.p.status)
@@ -390,67 +389,72 @@ __global__ void __launch_bounds__(RT, 2) attn_rows_kernel(AttnArgs a) {
     finish = lds[0] != 0;
     if (finish) {
       if (threadIdx.x == 0) sync_store(a.arrived + it.unit, 0u);
-      // every piece's reference and sum into LDS, one round trip for all of them; 16
-      // threads of a row then form its maximum and sum
-      float* refs = &merge[0][0];
-      float* sums = refs + it.pieces * ROWS;
-      for (int c = threadIdx.x; c < it.pieces * ROWS; c += RT)
-        buf_ld_shared2(ru, c / ROWS * Part<D>::kBytes + Part<D>::stats(c % ROWS), refs[c], sums[c]);
-      __syncthreads();
-      const int jr = threadIdx.x % ROWS, jp = threadIdx.x / ROWS;
-      float x = -INFINITY;
-      for (int c = jp; c < it.pieces; c += ROWS) x = fmaxf(x, refs[c * ROWS + jr]);
-      part_top[jp][jr] = x;
-      __syncthreads();
-      x = part_top[0][jr];
-#pragma unroll
-      for (int w = 1; w < ROWS; ++w) x = fmaxf(x, part_top[w][jr]);
-      float y = 0.f;
-      for (int c = jp; c < it.pieces; c += ROWS) {
-        const float r = refs[c * ROWS + jr], f = r == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(r - x);
-        refs[c * ROWS + jr] = f;
-        y += f * sums[c * ROWS + jr];
-      }
-      part_sum[jp][jr] = y;
-      __syncthreads();
-      // outputs: what is left of the threads beside the rows' own takes every n-th piece
+      // The threads of a row are CPR; what there are more of them than the tile's rows take
+      // (n times) share the pieces, each adding up every n-th one, eight of them (their
+      // references, sums and outputs) on their way at once.
       int rp = 1;
       while (rp < here) rp *= 2;
       const int n = RT / (CPR * rp), first_piece = threadIdx.x / (CPR * rp);
       mr = threadIdx.x / CPR % rp;
-      writes = mr < here && first_piece == 0;
+      top = -INFINITY;
+      total = 0.f;
 #pragma unroll
       for (int e = 0; e < 8; ++e) acc[e] = 0.f;
-      if (mr < here) {
-        top = part_top[0][mr];
-        total = 0.f;
+      if (mr < here)
+        for (int c0 = first_piece; c0 < it.pieces; c0 += 8 * n) {
+          float r[8], t[8];
+          f32x4 u[8], v[8];
 #pragma unroll
-        for (int w = 0; w < ROWS; ++w) {
-          top = fmaxf(top, part_top[w][mr]);
-          total += part_sum[w][mr];
-        }
-#pragma unroll 8
-        for (int c = first_piece; c < it.pieces; c += n) {
-          const uint32_t at = c * Part<D>::kBytes + Part<D>::out(mr, me);
-          const f32x4 u = load_coherent(ru, at), v = load_coherent(ru, at + 16);
-          const float f = refs[c * ROWS + mr];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            acc[e] += f * u[e];
-            acc[4 + e] += f * v[e];
+          for (int k = 0; k < 8; ++k) {  // pieces past the last one are out of the range: zeros
+            const uint32_t at = (c0 + k * n) * Part<D>::kBytes;
+            buf_ld_shared2(ru, at + Part<D>::stats(mr), r[k], t[k]);
+            u[k] = load_coherent(ru, at + Part<D>::out(mr, me));
+            v[k] = load_coherent(ru, at + Part<D>::out(mr, me + 4));
           }
+          float next = top;
+#pragma unroll
+          for (int k = 0; k < 8; ++k) {
+            if (c0 + k * n >= it.pieces) r[k] = -INFINITY;
+            next = fmaxf(next, r[k]);
+          }
+          const float base = next == -INFINITY ? 0.f : next, f0 = __builtin_amdgcn_exp2f(top - base);
+          total *= f0;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) acc[e] *= f0;
+#pragma unroll
+          for (int k = 0; k < 8; ++k) {
+            const float f = __builtin_amdgcn_exp2f(r[k] - base);
+            total += f * t[k];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              acc[e] += f * u[k][e];
+              acc[4 + e] += f * v[k][e];
+            }
+          }
+          top = next;
         }
-      }
+      writes = mr < here && first_piece == 0;
       if (n > 1) {
-        __syncthreads();
-        float* own = refs + threadIdx.x * 8;
+        float* own = &merge[0][0] + threadIdx.x * 10;
 #pragma unroll
         for (int e = 0; e < 8; ++e) own[e] = acc[e];
+        own[8] = top;
+        own[9] = total;
         __syncthreads();
-        if (writes)
-          for (int w = 1; w < n; ++w)
+        if (writes) {
+          for (int w = 1; w < n; ++w) top = fmaxf(top, own[w * CPR * rp * 10 + 8]);
+          const float base = top == -INFINITY ? 0.f : top;
+          total = 0.f;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) acc[e] += own[w * CPR * rp * 8 + e];
+          for (int e = 0; e < 8; ++e) acc[e] = 0.f;
+          for (int w = 0; w < n; ++w) {
+            const float* x = own + w * CPR * rp * 10;
+            const float f = __builtin_amdgcn_exp2f(x[8] - base);
+            total += f * x[9];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) acc[e] += f * x[e];
+          }
+        }
       }
     }
   }
