@@ -542,7 +542,8 @@ enum { VT_T_F16 = 0, VT_T_BF16 = 1, VT_T_F8E4M3 = 2 };
  * kernels look pages up once per 16 positions (smaller pages work, slower).
  * Table entries past a sequence's last position are not read. Sequences may
  * share pages that none of them writes. table, len, the scales and status need
- * 4-byte alignment only. */
+ * 4-byte alignment only. Up to 65536 sequences of fewer than 2^31 - 4095
+ * positions. */
 typedef struct vt_paged_kv {
   void* k;
   void* v;
@@ -570,7 +571,8 @@ typedef struct vt_paged_kv {
  * q_begin is device, [n_seqs + 1], ascending from 0 to at most n_tok; NULL
  * stands for one token per sequence (row s is sequence s's; n_tok = n_seqs).
  * Rows behind the last sequence are padding: nothing is read or written for
- * them. A sequence of length 0 is an idle slot of the batch. */
+ * them. A sequence of length 0 is an idle slot of the batch. Up to 2^20 rows
+ * and 1024 query heads. */
 typedef struct vt_paged_io {
   int32_t type;
   int32_t n_tok;
@@ -605,7 +607,7 @@ vt_status vt_paged_append(const vt_paged_kv* kv, const vt_paged_io* io, float ro
                           uint32_t flags, void* stream);
 
 /* Bytes of device workspace that vt_paged_decode_attn and vt_paged_chunk_attn
- * need (65 MiB at head_dim 128; the same for every batch at one head_dim). It
+ * need (66 MiB at head_dim 128; the same for every batch at one head_dim). It
  * must be zero-filled once before its first use by these two entry points (it
  * is theirs alone: no other entry point's workspace); they leave its
  * synchronisation words zero after every call. One workspace must not be used
@@ -630,7 +632,7 @@ vt_status vt_paged_decode_attn(const vt_paged_kv* kv, const vt_paged_io* io, flo
 /* The same for a chunk of new tokens per sequence (io->q_begin; NULL as
  * above): the token at position p attends to positions 0..p, the last
  * ``window`` of them if window > 0. Chunks of any lengths may be mixed. Where
- * the batch has more than 24 rows (new tokens x query heads per KV head) per
+ * the batch has more than 32 rows (new tokens x query heads per KV head) per
  * sequence, the weights enter the product with the values rounded once to the
  * activations' type. */
 vt_status vt_paged_chunk_attn(const vt_paged_kv* kv, const vt_paged_io* io, float scale,

@@ -198,6 +198,8 @@ vt_status check_pool(const vt_paged_kv& kv, const vt_paged_io& io) {
       return fail(VT_ERR_ARG, "%s %lld is below head_dim or above 2^40", x.name, static_cast<long long>(x.v));
     if (x.v * elem % 16) return fail(VT_ERR_ALIGN, "%s is not a multiple of 16 bytes", x.name);
   }
+  if ((static_cast<int64_t>(kv.n_pages) - 1) > (int64_t(1) << 46) / std::max<int64_t>(kv.page_stride * elem, 1))
+    return fail(VT_ERR_UNSUPPORTED, "pages span more than 2^46 bytes");
   // a tile's rows are addressed by 32-bit offsets
   if (kv.slot_stride * elem > (int64_t(1) << 24))
     return fail(VT_ERR_UNSUPPORTED, "slot_stride of more than 2^24 bytes");
@@ -241,30 +243,28 @@ pg::Pool pool_of(const vt_paged_kv& kv) {
   p.shift = shift;
   p.mask = kv.page_size - 1;
   p.capacity = static_cast<int32_t>(
-      std::min<int64_t>(static_cast<int64_t>(kv.max_pages) * kv.page_size, INT32_MAX));
+      std::min<int64_t>(static_cast<int64_t>(kv.max_pages) * kv.page_size, pg::kMaxPositions));
   p.n_kv = kv.n_kv_heads;
   p.n_seqs = kv.n_seqs;
   return p;
 }
 
-// Bytes of one partial result: its rows' outputs, references and sums.
-size_t part_bytes(int rows, int head_dim) { return static_cast<size_t>(rows) * (head_dim + 2) * sizeof(float); }
-
 // Rows of an attention tile, by the mean rows of a sequence (what else the host could
 // know of a batch is on the device): 16 (attn_rows_kernel), 64 or 128 (attn_chunk_kernel).
 // All take every batch; keys and values pass once per tile and a tile's rows cost the
-// same whether they are there or not. Measured with 16 / 64 / 128: one sequence of 17 rows
-// over 17 positions 5.2 / 6.5 / 6.1 us; 16 sequences of 26 rows on average over up to
-// 4099 positions 58.6 / 54.6 / 77; one of 4096 rows 617 / 239 / 206.
+// same whether they are there or not. Measured with 16 / 64 / 128 (us), rows per sequence:
+// 16 sequences of 4096 positions, 8 heads: 16 rows 55 / 63 / 74, 32 rows 62 / 65 / 75, 64 rows 96 /
+// 65 / 76, 128 rows 164 / 88 / 78; with 8-bit caches 29 / 54 / 62, 35 / 53 / 61, 58 / 54 / 62, 107 / 85 / 67;
+// one of 32768: 32 rows 32 / 42 / 56, 64 rows 48 / 43 / 57; one prompt of 4096 rows 617 / 239 / 182.
 int tile_rows(const vt_paged_kv& kv, const vt_paged_io& io) {
   if (!io.q_begin) return 16;
   const double rows = static_cast<double>(io.n_tok) * (io.n_q_heads / kv.n_kv_heads) / kv.n_seqs;
-  return rows <= 24 ? 16 : (rows <= 64 ? 64 : 128);
+  return rows <= 32 ? 16 : (rows <= 64 ? 64 : 128);
 }
 
 // Fewer than 2 * kTarget pieces of the largest tile: the same for every batch.
 size_t workspace_bytes(const vt_paged_kv& kv) {
-  return pg::kSyncBytes + 2 * static_cast<size_t>(pg::kTarget) * part_bytes(128, kv.head_dim);
+  return pg::kSyncBytes + 2 * static_cast<size_t>(pg::kTarget) * pg::part_bytes(128, kv.head_dim);
 }
 
 vt_status attend(const vt_paged_kv* kv, const vt_paged_io* io, float scale, int32_t window, void* ws, size_t ws_bytes,
@@ -302,6 +302,10 @@ vt_status attend(const vt_paged_kv* kv, const vt_paged_io* io, float scale, int3
   const int tile = tile_rows(*kv, *io);
   a.target = tile == 128 ? pg::kTarget : pg::kTarget / 2;
   a.min_blocks = tile == 16 ? 2 : 4;
+  const int64_t grid = pg::grid_of(a, tile);
+  if (grid >= (int64_t(1) << 24))  // 2^32 threads
+    return fail(VT_ERR_UNSUPPORTED, "%lld tiles of rows: fewer tokens, heads or sequences per call",
+                static_cast<long long>(grid));
   hipError_t e = tile == 16 ? pg::launch_rows(a, io->type, f8, kv->head_dim, s)
                             : pg::launch_chunk(a, io->type, f8, kv->head_dim, tile, s);
   return e == hipSuccess ? VT_OK : fail(VT_ERR_HIP, "attention launch: %s", hipGetErrorString(e));
@@ -340,9 +344,12 @@ extern "C" vt_status vt_paged_append(const vt_paged_kv* kv, const vt_paged_io* i
   a.n_tok = io->n_tok;
   a.n_q = io->n_q_heads;
   pg::Freq f{};
-  if (rope_base > 0.f)
-    for (int i = 0; i < d / 2; ++i)
-      f.rev[i] = std::pow(static_cast<double>(rope_base), -2.0 * i / static_cast<double>(d)) * 0.15915494309189535;
+  if (rope_base > 0.f) {
+    // powers by products with 64 bits of mantissa: off by 2^-57 at most, in the time of one pow
+    const long double step = std::pow(static_cast<long double>(rope_base), -2.0L / static_cast<long double>(d));
+    long double rev = 0.159154943091895335768883763372514362L;  // 1 / (2 pi)
+    for (int i = 0; i < d / 2; ++i, rev *= step) f.rev[i] = static_cast<double>(rev);
+  }
   // heads of a token over several workgroups only while there are few tokens
   const int halves = flags & VT_ROPE_HALVES ? 1 : 0, hl = pg::CT / (static_cast<int>(d) / 8 >> halves);
   const int rows = 2 * kv->n_kv_heads + (io->q ? io->n_q_heads : 0), parts = (rows + hl - 1) / hl;

@@ -79,7 +79,7 @@ struct Pool {
   const float* k_scale;
   const float* v_scale;
   int32_t n_pages, shift, mask;  // page_size = 1 << shift = mask + 1
-  int32_t capacity;              // positions a table row can name (at most 2^31 - 1)
+  int32_t capacity;              // positions a table row can name, at most kMaxPositions
   int32_t n_kv, n_seqs;
 };
 
@@ -213,9 +213,12 @@ struct Plan {
 
   // The pieces of a unit are joined by one workgroup, in time that grows with their number.
   // A 16-row tile's partial results are small: 128 of them come in a few round trips. Those of
-  // the larger tiles are as large as what two stages load: as many pieces as a piece has blocks.
+  // the larger tiles are as large as what one or two stages load: about as many pieces as a
+  // piece has blocks, or (64 rows) twice that (32 rows over 32768 positions 43.3 -> 41.7 us with twice
+  // as many, 128 rows 57.2 -> 70).
   __device__ __forceinline__ int pieces(int blocks) const {
-    const int cap = ROWS == 16 ? 128 : max(1, static_cast<int>(sqrtf(static_cast<float>(blocks))));
+    const float root = sqrtf(static_cast<float>(blocks));
+    const int cap = ROWS == 16 ? 128 : max(1, static_cast<int>(ROWS == 64 ? 2.f * root : root));
     return min(cap, max(1, (blocks + most - 1) / most));
   }
 
@@ -327,14 +330,24 @@ __device__ __forceinline__ bool next_item(const AttnArgs& a, int i, Item& t, int
   return true;
 }
 
-// Workgroups that cover a batch's items, one each: a cut into pieces of X or more blocks adds
-// at most N / X <= target to the units. The rest ends at once.
-inline uint32_t grid_of(const AttnArgs& a, int64_t tiles, int keys) {
+// ---- host side, in paged.hip -------------------------------------------------
+// Positions of a sequence: the end of the block behind the last one is still an int.
+constexpr int32_t kMaxPositions = INT32_MAX - 4095;
+
+// Most bytes of one partial result: its rows' outputs, and a reference and a sum for each of the
+// two lanes that hold a row.
+constexpr size_t part_bytes(int rows, int head_dim) { return static_cast<size_t>(rows) * (head_dim + 4) * 4; }
+
+// Workgroups that cover a batch's items, one each, on tiles of ``rows`` rows: a cut into pieces of
+// X or more blocks adds at most N / X <= target to the units. The rest ends at once.
+inline int64_t grid_of(const AttnArgs& a, int rows) {
+  const int64_t tiles = a.q_begin ? static_cast<int64_t>(a.n_tok) * a.group / rows + a.p.n_seqs
+                                  : static_cast<int64_t>(a.p.n_seqs) * ((a.group + rows - 1) / rows);
+  const int keys = rows == 16 ? 128 : 64;  // of a block
   const int64_t units = tiles * a.p.n_kv, blocks = (static_cast<int64_t>(a.p.capacity) + keys - 1) / keys;
-  return static_cast<uint32_t>(blocks <= 1 ? units : (units * blocks < units + a.target ? units * blocks : units + a.target));
+  return units * blocks < units + a.target ? units * blocks : units + a.target;
 }
 
-// ---- host side, in paged.hip -------------------------------------------------
 // Work items aimed at by the largest tiles, two workgroups of which a compute unit holds.
 // The smaller tiles aim at half of that, one per compute unit: their pieces wait for
 // memory, and longer ones have less to start, to end and to join (64 sequences of 2000-4097

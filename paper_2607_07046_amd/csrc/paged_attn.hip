@@ -47,6 +47,7 @@ __device__ __forceinline__ f32x4 load_coherent(rsrc_t r, uint32_t off) {
 template <int D>
 struct Part {
   static constexpr uint32_t kBytes = ROWS * (D + 2) * 4;
+  static_assert(kBytes <= part_bytes(ROWS, D), "");
   static __device__ __forceinline__ uint32_t out(int row, int e) { return (row * D + e) * 4; }
   static __device__ __forceinline__ uint32_t stats(int row) { return (ROWS * D + 2 * row) * 4; }
 };
@@ -485,9 +486,8 @@ hipError_t launch_rows(const AttnArgs& a, int type, bool f8, int head_dim, hipSt
     return big ? attn_rows_kernel<T, false, 64, true> : attn_rows_kernel<T, false, 64, false>;
   };
   auto* kernel = type == VT_T_F16 ? pick(Half{}) : pick(BFloat{});
-  const int64_t tiles = a.q_begin ? static_cast<int64_t>(a.n_tok) * a.group / ROWS + a.p.n_seqs
-                                  : static_cast<int64_t>(a.p.n_seqs) * ((a.group + ROWS - 1) / ROWS);
-  hipLaunchKernelGGL(kernel, dim3(grid_of(a, tiles, RB)), dim3(RT), 0, s, a);
+  static_assert(ROWS == 16 && RB == 128, "grid_of counts these");
+  hipLaunchKernelGGL(kernel, dim3(static_cast<uint32_t>(grid_of(a, ROWS))), dim3(RT), 0, s, a);
   return hipGetLastError();
 }
 

@@ -96,6 +96,7 @@ struct Chunk {
   // a partial result of a wave: [register quad][lane][4], then a reference and a sum per lane
   static constexpr int QUADS = D / 8;
   static constexpr uint32_t PART = RGW * kWave * (QUADS * 16 + 8);
+  static_assert(PART <= part_bytes(ROWS, D) && KS == 64, "");
 };
 
 template <class T, bool F8, int D, bool BIG, int KG>
@@ -549,8 +550,9 @@ __global__ void __launch_bounds__(CTH, 2) attn_chunk_kernel(AttnArgs a) {
   }
   sum += __shfl_xor(sum, 32, kWave);
 
-  if constexpr (KG == 2) {
-    // the second half of the waves leave their results in LDS, in register order
+  // the second half of the waves' results, left in LDS in register order, into the first's
+  auto merge = [&]() {
+    if constexpr (KG == 1) return;
     __syncthreads();
     float* part = reinterpret_cast<float*>(smem) + wr * (D / 2 + 2) * kWave + lane;
     if (kg == 1) {
@@ -572,7 +574,8 @@ __global__ void __launch_bounds__(CTH, 2) attn_chunk_kernel(AttnArgs a) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[m][i] = o[m][i] * f0 + part[(m * 16 + i) * kWave] * f1;
     }
-  }
+  };
+  merge();
 
   if (it.pieces > 1) {
     const rsrc_t ru = make_rsrc(reinterpret_cast<char*>(a.part) + static_cast<int64_t>(it.slot) * C::PART,
@@ -600,29 +603,35 @@ __global__ void __launch_bounds__(CTH, 2) attn_chunk_kernel(AttnArgs a) {
     // the last piece to arrive joins them all, in their order
     if (lds[0] == 0) return;
     if (threadIdx.x == 0) sync_store(a.arrived + it.unit, 0u);
-    if (kg == 0) {
-      ref = -INFINITY;
-      sum = 0.f;
+    // two pieces' numbers on their way at once, the groups of waves taking turns
+    ref = -INFINITY;
+    sum = 0.f;
 #pragma unroll
-      for (int m = 0; m < NM; ++m) o[m] = f32x16{};
-      for (int c = 0; c < it.pieces; ++c) {
-        float r, t;
-        buf_ld_shared2(ru, c * C::PART + stats, r, t);
-        u32x4 x[C::QUADS];
+    for (int m = 0; m < NM; ++m) o[m] = f32x16{};
+    for (int c = 2 * kg; c < it.pieces; c += 2 * KG) {
+      float r[2], t[2];
+      u32x4 x[2][C::QUADS];
 #pragma unroll
-        for (int i = 0; i < C::QUADS; ++i)
-          x[i] = __builtin_amdgcn_raw_buffer_load_b128(ru, c * C::PART + quad(i), 0, kCoherent);
-        const float top = fmaxf(ref, r), base = top == -INFINITY ? 0.f : top;
-        const float f0 = __builtin_amdgcn_exp2f(ref - base), f1 = __builtin_amdgcn_exp2f(r - base);
-        ref = top;
-        sum = sum * f0 + t * f1;
+      for (int k = 0; k < 2; ++k) {  // a piece past the last one is out of the range: zeros
+        buf_ld_shared2(ru, (c + k) * C::PART + stats, r[k], t[k]);
 #pragma unroll
         for (int i = 0; i < C::QUADS; ++i)
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            o[i / 4][i % 4 * 4 + e] = o[i / 4][i % 4 * 4 + e] * f0 + f1 * __builtin_bit_cast(f32x4, x[i])[e];
+          x[k][i] = __builtin_amdgcn_raw_buffer_load_b128(ru, (c + k) * C::PART + quad(i), 0, kCoherent);
       }
+      if (c + 1 >= it.pieces) r[1] = -INFINITY;
+      const float top = fmaxf(ref, fmaxf(r[0], r[1])), base = top == -INFINITY ? 0.f : top;
+      const float f = __builtin_amdgcn_exp2f(ref - base), f0 = __builtin_amdgcn_exp2f(r[0] - base),
+                  f1 = __builtin_amdgcn_exp2f(r[1] - base);
+      ref = top;
+      sum = sum * f + t[0] * f0 + t[1] * f1;
+#pragma unroll
+      for (int i = 0; i < C::QUADS; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          o[i / 4][i % 4 * 4 + e] = o[i / 4][i % 4 * 4 + e] * f + f0 * __builtin_bit_cast(f32x4, x[0][i])[e] +
+                                    f1 * __builtin_bit_cast(f32x4, x[1][i])[e];
     }
+    merge();
   }
   if (kg != 0 || !there) return;
   const float vs = F8 && a.p.v_scale ? a.p.v_scale[it.head] : 1.f;
@@ -642,17 +651,15 @@ __global__ void __launch_bounds__(CTH, 2) attn_chunk_kernel(AttnArgs a) {
 
 hipError_t launch_chunk(const AttnArgs& a, int type, bool f8, int head_dim, int tile, hipStream_t s) {
   const bool big = a.p.mask + 1 >= 16;
-  int rows = 0, shared = 0;
+  int shared = 0;
   auto pick = [&](auto X, auto F, auto B, auto DD) -> void (*)(AttnArgs) {
     using T = decltype(X);
     constexpr int D = decltype(DD)::value;
     constexpr bool f = decltype(F)::value, b = decltype(B)::value;
     if (tile == 64) {
-      rows = Chunk<D, 2>::ROWS;
       shared = std::max<int>(Chunk<D, 2>::LDS, Chunk<D, 2>::RGW * (D / 2 + 2) * kWave * 4);
       return attn_chunk_kernel<T, f, D, b, 2>;
     }
-    rows = Chunk<D, 1>::ROWS;
     shared = Chunk<D, 1>::LDS;
     return attn_chunk_kernel<T, f, D, b, 1>;
   };
@@ -665,10 +672,9 @@ hipError_t launch_chunk(const AttnArgs& a, int type, bool f8, int head_dim, int 
   };
   auto pick1 = [&](auto X) { return f8 ? pick2(X, std::true_type{}) : pick2(X, std::false_type{}); };
   auto* kernel = type == VT_T_F16 ? pick1(Half{}) : pick1(BFloat{});
-  const int64_t tiles = static_cast<int64_t>(a.n_tok) * a.group / rows + a.p.n_seqs;
   hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, shared);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(kernel, dim3(grid_of(a, tiles, KS)), dim3(CTH), shared, s, a);
+  hipLaunchKernelGGL(kernel, dim3(static_cast<uint32_t>(grid_of(a, tile))), dim3(CTH), shared, s, a);
   return hipGetLastError();
 }
 

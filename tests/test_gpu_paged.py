@@ -410,6 +410,25 @@ def test_offsets_past_32_bits():
     assert int(b.status) == 0
 
 
+@pytest.mark.parametrize("new", [1, 3, 200])
+def test_windows_at_the_largest_positions(new):
+    """Attention does not depend on where a window lies: the same one at the end of the range of
+    positions, its other pages long gone, gives the same bits."""
+    b = Batch([30000], [new], kv_heads=2, group=2, d=64, page=32768, window=100)
+    b.attend()
+    b.check(rounded=True)
+    out, lse = b.out.clone(), b.lse.clone()
+    far = 65534
+    table = torch.full((1, far + 1), -1, dtype=torch.int32, device="cuda")
+    table[0, far] = b.table[0, 0]
+    b.table, b.max_pages = table, far + 1
+    b.len += far * 32768
+    ws = b.workspace()
+    vt.vt_paged_chunk_attn(b.kv(ld_table=far + 1), b.io(), 0.0, 100, ws.data_ptr(), ws.numel(), None)
+    torch.cuda.synchronize()
+    assert torch.equal(out, b.out) and torch.equal(lse, b.lse) and int(b.status) == 0
+
+
 def test_contiguous_cache_of_the_layer():
     """The cache that vt_layer_prefill_chunk fills, read as a paged one: slots of a head side by
     side, table 0, 1, 2, .. ; its last page is not whole."""
@@ -527,6 +546,18 @@ def test_one_workspace_for_many_shapes():
         b = Batch(lens, new, kv_heads=1, group=group, d=d, page=32)
         b.attend(ws)
         b.check(rounded=new is not None)
+
+
+def test_partial_results_stay_in_the_workspace():
+    """505 units, each a little too long for one piece: the most pieces that a split comes to."""
+    b = Batch([5600] * 101, [128] * 101, kv_heads=5, group=1, d=64, page=64)
+    n = b.workspace().numel()
+    ws = torch.zeros(n + (1 << 20), dtype=torch.uint8, device="cuda")
+    ws[n:] = 0xA5
+    vt.vt_paged_chunk_attn(b.kv(), b.io(), 0.0, 0, ws.data_ptr(), n, None)
+    torch.cuda.synchronize()
+    assert bool((ws[n:] == 0xA5).all()) and not ws[:8192].any()
+    b.check(rounded=True)
 
 
 def test_two_streams_with_a_workspace_each():

@@ -65,6 +65,8 @@ BOTH = [  # refused by append and attention alike
     (vt.VT_ERR_ARG, dict(head_stride=0), {}),
     (vt.VT_ERR_UNSUPPORTED, dict(slot_stride=1 << 24), {}),
     (vt.VT_ERR_ARG, dict(page_stride=1 << 41), {}),
+    (vt.VT_ERR_UNSUPPORTED, dict(page_stride=1 << 40, n_pages=65), {}),
+    (vt.VT_ERR_UNSUPPORTED, dict(n_pages=2 ** 31 - 1, page_stride=1 << 16), {}),
     (vt.VT_ERR_ARG, dict(n_pages=0), {}),
     (vt.VT_ERR_ARG, dict(page_size=0), {}),
     (vt.VT_ERR_ARG, dict(page_size=24), {}),
@@ -132,6 +134,11 @@ def test_append_refuses_flags():
     (vt.VT_ERR_ALIGN, {}, dict(ws=P + 4)), (vt.VT_ERR_WORKSPACE, {}, dict(ws_bytes=4096))])
 def test_attention_refuses(call, status, i, a):
     refused(status, call, kv(), io(**i), **a)
+
+
+def test_more_tiles_than_a_launch_has():
+    refused(vt.VT_ERR_UNSUPPORTED, decode, kv(n_seqs=65536, n_kv_heads=256), io(n_tok=65536, n_q_heads=256, ld_qr=1 << 14,
+                                                                              ld_out=1 << 14))
 
 
 def test_decode_refuses_chunks():
