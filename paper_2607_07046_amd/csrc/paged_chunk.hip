@@ -1,9 +1,10 @@
 // Attention of many query rows over a paged cache: chunks of prompts.
 //
 // A workgroup of four waves takes a tile of rows of one KV head (a row is one query
-// head of one token, the heads that share the KV head side by side), a wave 32 rows. Keys and values come in stages of 64 into LDS, once for all rows of
-// the tile: 16-bit caches straight from memory, 8-bit ones through registers, where
-// they are widened. Both products run as
+// head of one token, the heads that share the KV head side by side), a wave 32 rows.
+// Keys and values come in stages of 64 into LDS, once for all rows of the tile: 16-bit
+// caches straight from memory, 8-bit ones through registers, where they are widened. Both
+// products run as
 //   S^T = K Q^T, O^T = V^T P^T on 32 x 32 x 16 matrix instructions:
 // a lane has one row (l % 32) of every result, so the softmax needs other lanes only for
 // a new maximum, and its weights are the second product's operand as they stand, if
@@ -355,21 +356,31 @@ __global__ void __launch_bounds__(CTH, 2) attn_chunk_kernel(AttnArgs a) {
   // One block by itself, from key p0 on, with a new reference: one that some rows of the wave
   // do not see whole, or whose scores ask for it; gone: its keys on bad pages.
   auto single = [&](const char* S, int p0, uint32_t gone) {
+    const bool whole = p0 >= full_lo && p0 + 32 <= full_hi && gone == 0;
     f32x16 s = f32x16{};
+    {
+      u32x4 kf[NK];
 #pragma unroll
-    for (int c = 0; c < NK; ++c) s = T::mfma32(kfrag(S, c), qf[c], s);
+      for (int c = 0; c < NK; ++c) kf[c] = kfrag(S, c);
+      __builtin_amdgcn_sched_barrier(0);  // all of them on their way before the first product
+#pragma unroll
+      for (int c = 0; c < NK; ++c) s = T::mfma32(kf[c], qf[c], s);
+    }
     u32x4 pf[2];
-    const uint32_t mine = span(p0, klo, khi), sees = own16(mine & ~gone);
+    uint32_t used = 0xFFFFu;  // of the lane's keys
+    if (!whole) {
+      const uint32_t mine = span(p0, klo, khi), sees = own16(mine & ~gone);
 #pragma unroll
-    for (int i = 0; i < 16; ++i)
-      if (!(sees >> i & 1)) s[i] = -INFINITY;
-    if (__builtin_amdgcn_ballot_w64(there && (mine & gone)) != 0 && a.p.status)
-      sync_or(a.p.status, VT_PAGED_BAD_PAGE);
+      for (int i = 0; i < 16; ++i)
+        if (!(sees >> i & 1)) s[i] = -INFINITY;
+      if (__builtin_amdgcn_ballot_w64(there && (mine & gone)) != 0 && a.p.status)
+        sync_or(a.p.status, VT_PAGED_BAD_PAGE);
+      used = own16(span(p0, any_lo, any_hi) & ~gone);
+    }
     refer(largest(s));
     weigh(s, pf, sum);
     // values that no row of the wave sees stay out of the product even if they are
     // infinite
-    const uint32_t used = own16(span(p0, any_lo, any_hi) & ~gone);
     auto seen = [&](int m, int b, uint32_t keys) {  // a fragment's values of these of the lane's keys
       u32x4 z = vfrag(S, m, b);
 #pragma unroll
@@ -377,42 +388,50 @@ __global__ void __launch_bounds__(CTH, 2) attn_chunk_kernel(AttnArgs a) {
         z[w] &= (keys >> (8 * b + 2 * w) & 1 ? 0xFFFFu : 0u) | (keys >> (8 * b + 2 * w + 1) & 1 ? 0xFFFF0000u : 0u);
       return z;
     };
-    uint32_t odd = 0;  // a zero half among the exponents' complements: an infinity or a NaN
-#pragma unroll
-    for (int m = 0; m < NM; ++m)
+    if (!whole) {
+      uint32_t odd = 0;  // a zero half among the exponents' complements: an infinity or a NaN
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
-        const u32x4 z = seen(m, b, used);
+        u32x4 z[NM];
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
-          const uint32_t c = ~z[w] & T::kExp;
-          odd |= (c - 0x00010001u) & ~c & 0x80008000u;
-        }
+        for (int m = 0; m < NM; ++m) z[m] = seen(m, b, used);
+#pragma unroll
+        for (int m = 0; m < NM; ++m)
+#pragma unroll
+          for (int w = 0; w < 4; ++w) {
+            const uint32_t c = ~z[m][w] & T::kExp;
+            odd |= (c - 0x00010001u) & ~c & 0x80008000u;
+          }
         __builtin_amdgcn_sched_barrier(0);
       }
-    if (__builtin_amdgcn_ballot_w64(odd != 0) != 0) {
-      // where some rows see an infinite or NaN value and others do not, each row gets a
-      // product of its own, with what it does not see set to zero
+      if (__builtin_amdgcn_ballot_w64(odd != 0) != 0) {
+        // where some rows see an infinite or NaN value and others do not, each row gets a
+        // product of its own, with what it does not see set to zero
 #pragma unroll
-      for (int m = 0; m < NM; ++m) {
-        f32x16 keep = o[m];
+        for (int m = 0; m < NM; ++m) {
+          f32x16 keep = o[m];
 #pragma unroll 1
-        for (int c = 0; c < 32; ++c) {
-          const uint32_t row =
-              own16(span(p0, __builtin_amdgcn_readlane(klo, c), __builtin_amdgcn_readlane(khi, c)) & ~gone);
-          f32x16 r = o[m];
+          for (int c = 0; c < 32; ++c) {
+            const uint32_t row =
+                own16(span(p0, __builtin_amdgcn_readlane(klo, c), __builtin_amdgcn_readlane(khi, c)) & ~gone);
+            f32x16 r = o[m];
 #pragma unroll
-          for (int b = 0; b < 2; ++b) r = T::mfma32(seen(m, b, row), pf[b], r);
-          if (ql == c) keep = r;
+            for (int b = 0; b < 2; ++b) r = T::mfma32(seen(m, b, row), pf[b], r);
+            if (ql == c) keep = r;
+          }
+          o[m] = keep;
         }
-        o[m] = keep;
+        return;
       }
-      return;
     }
 #pragma unroll
-    for (int b = 0; b < 2; ++b)
+    for (int b = 0; b < 2; ++b) {
+      u32x4 z[NM];
 #pragma unroll
-      for (int m = 0; m < NM; ++m) o[m] = T::mfma32(seen(m, b, used), pf[b], o[m]);
+      for (int m = 0; m < NM; ++m) z[m] = seen(m, b, used);
+#pragma unroll
+      for (int m = 0; m < NM; ++m) o[m] = T::mfma32(z[m], pf[b], o[m]);
+    }
   };
 
   if (stages > 0) {
