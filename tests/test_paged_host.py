@@ -1,9 +1,13 @@
 """Refusals of the paged-cache entry points, none of which reaches the GPU, and
-their workspace size."""
+their workspace size; and the compiler's output around the loads into LDS."""
 import math
+import os
+import re
+import subprocess
 
 import pytest
 
+from paper_2607_07046_amd import build
 from paper_2607_07046_amd import voltron as vt
 
 P = 0x10000  # an aligned address that nothing reads
@@ -155,3 +159,18 @@ def test_workspace_size():
     assert lib.vt_paged_append(None, None, 0.0, 0, None) == vt.VT_ERR_ARG
     assert lib.vt_paged_decode_attn(None, None, 0.0, 0, None, 0, None) == vt.VT_ERR_ARG
     assert lib.vt_paged_chunk_attn(None, None, 0.0, 0, None, 0, None) == vt.VT_ERR_ARG
+
+
+def test_direct_loads_keep_their_target(tmp_path):
+    """A load into LDS takes its target from m0: in the compiler's output each one directly
+    follows the write of m0 and the wait state that it needs, and nothing else uses m0."""
+    source, out = os.path.join(build.CSRC, "paged_chunk.hip"), tmp_path / "paged_chunk.s"
+    subprocess.run([build.HIPCC, *build.FLAGS, "-I", os.path.join(build.ROOT, "include"), "-I", build.CSRC,
+                    "--cuda-device-only", "-S", source, "-o", str(out)], check=True, capture_output=True)
+    lines = [t for t in (line.split(";")[0].strip() for line in out.read_text().split("\n"))
+             if t and not t.startswith(".") and not t.endswith(":")]
+    loads = [i for i, t in enumerate(lines) if t.startswith("global_load_lds")]
+    assert loads
+    for i in loads:
+        assert re.match(r"s_mov_b32 m0, s\d+$", lines[i - 2]) and lines[i - 1] == "s_nop 0", lines[i - 2:i + 1]
+    assert sum(re.search(r"\bm0\b", t) is not None for t in lines) == len(loads)
