@@ -623,9 +623,10 @@ vt_status vt_paged_workspace_size(const vt_paged_kv* kv, const vt_paged_io* io, 
  * weights enter the product with the values as two numbers of the activations'
  * type, their rounding and its remainder. A query that sees no key (an idle
  * slot) gets out 0 and lse -infinity. Values and keys outside the visible
- * positions, and of bad pages, have no influence whatever they hold. With
- * ``lse`` the results of caches that hold different positions of one sequence
- * can be joined. */
+ * positions, and of bad pages, have no influence whatever they hold; a visible
+ * value that is infinite or NaN leaves its element of the output infinite or
+ * NaN, not always the one that the formula has. With ``lse`` the results of
+ * caches that hold different positions of one sequence can be joined. */
 vt_status vt_paged_decode_attn(const vt_paged_kv* kv, const vt_paged_io* io, float scale,
                                int32_t window, void* ws, size_t ws_bytes, void* stream);
 

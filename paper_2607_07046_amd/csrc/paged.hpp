@@ -201,12 +201,13 @@ struct Share {
 // nothing depends on what the host knows of them: with N key blocks in all (over
 // tiles and heads), units longer than X = max(min_blocks, N / target) blocks are cut
 // into pieces of about equal size. Fewer than ``target`` units are cut, into fewer than
-// 2 * target pieces in all, whatever the lengths: that sizes counters and partials.
+// 2 * target pieces in all, whatever the lengths: that sizes counters and partials. (X may
+// become longer, see fit.)
 // Up to NT sequences a thread keeps its own one's length from the only load of it.
 template <int ROWS, int KEYS, int NT>
 struct Plan {
   int32_t per;     // sequences per thread
-  int32_t most;    // X
+  int32_t most;    // X, longest piece in blocks
   int32_t base[3]; // items, cut units and pieces of them before this thread's sequences
   int32_t total;   // items in all
   Seq mine;        // this thread's sequence, if it has one only
@@ -216,10 +217,12 @@ struct Plan {
   // the larger tiles are as large as what one or two stages load: about as many pieces as a
   // piece has blocks, or (64 rows) twice that (32 rows over 32768 positions 43.3 -> 41.7 us with twice
   // as many, 128 rows 57.2 -> 70).
-  __device__ __forceinline__ int pieces(int blocks) const {
+  static __device__ __forceinline__ int most_pieces(int blocks) {
     const float root = sqrtf(static_cast<float>(blocks));
-    const int cap = ROWS == 16 ? 128 : max(1, static_cast<int>(ROWS == 64 ? 2.f * root : root));
-    return min(cap, max(1, (blocks + most - 1) / most));
+    return ROWS == 16 ? 128 : max(1, static_cast<int>(ROWS == 64 ? 2.f * root : root));
+  }
+  __device__ __forceinline__ int pieces(int blocks) const {
+    return min(most_pieces(blocks), max(1, (blocks + most - 1) / most));
   }
 
   __device__ __forceinline__ Seq seq(const AttnArgs& a, int s) const { return per == 1 ? mine : sequence(a, s); }
@@ -229,6 +232,61 @@ struct Plan {
     most = max(a.min_blocks, static_cast<int32_t>(ceilf(fminf(n * 1.0001f / static_cast<float>(a.target), 1e9f))));
   }
 
+  // ``target`` items run at once, so X times the rounds of them is about the time: X times 5/4, 3/2 or
+  // 2 is taken where its pieces fit into so many fewer rounds (16 sequences of 2056-4099 positions,
+  // 8 heads of one or two tiles 59.5 -> 54 us, 12 ragged ones 45.2 -> 37.8, three chunks of 256 tokens
+  // 136 -> 117). The counts are estimates: quotients are rounded, and a thread's share ends
+  // at 1023 (ten bits, so that a wave's sum has 16). The cut stays the lengths' alone.
+  __device__ __forceinline__ int longer(int i) const {  // less than 2^31: X is at most 10^9
+    return i == 0 ? most : (i == 1 ? most + most / 4 : (i == 2 ? most + most / 2 : 2 * most));
+  }
+  struct Tries {
+    float items[4];
+  };
+  __device__ __forceinline__ void count(const AttnArgs& a, const Share<ROWS, KEYS>& h, Tries& t) const {
+    const float n = static_cast<float>(h.tiles * a.p.n_kv), b = static_cast<float>(h.blocks);
+    const float top = static_cast<float>(most_pieces(h.blocks));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float p = ceilf(b * __builtin_amdgcn_rcpf(static_cast<float>(longer(i))) - 1e-3f);
+      t.items[i] += n * fminf(top, fmaxf(p, 1.f));
+    }
+  }
+  __device__ __forceinline__ void fit(const AttnArgs& a, const Tries& t) {
+    float least = 0.f;
+    int best = most;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int x = longer(i);
+      const float time = ceilf(t.items[i] / static_cast<float>(a.target)) * static_cast<float>(x);
+      if (i == 0 || time < least) {
+        least = time;
+        best = x;
+      }
+    }
+    most = __builtin_amdgcn_readfirstlane(best);
+  }
+
+  // Whether pieces may fit better: some units are cut, into more items than run at once, and not
+  // into so many that one round more or less makes no difference.
+  __device__ __forceinline__ bool uneven(const AttnArgs& a, int items, int cut_pieces) const {
+    return cut_pieces > 0 && items > a.target && items <= 4 * a.target;
+  }
+
+  // The items, cut units and pieces of them before this thread's sequences; the counts of all.
+  __device__ __forceinline__ void count_all(const AttnArgs& a, int s0, int s1, int (&tot)[3], int* lds) {
+#pragma unroll
+    for (int i = 0; i < 3; ++i) base[i] = 0;
+    for (int s = s0; s < s1; ++s) {
+      const Share<ROWS, KEYS> h(a, seq(a, s));
+      const int units = h.tiles * a.p.n_kv, pc = pieces(h.blocks);
+      base[0] += units * pc;
+      base[1] += pc > 1 ? units : 0;
+      base[2] += pc > 1 ? units * pc : 0;
+    }
+    scan3<NT>(base, tot, lds);
+  }
+
   __device__ __forceinline__ void make(const AttnArgs& a, int* lds) {
     per = (a.p.n_seqs + NT - 1) / NT;
     if (a.p.n_seqs == 1) {  // every thread has it, and nothing is to be summed up
@@ -236,7 +294,14 @@ struct Plan {
       const Share<ROWS, KEYS> h(a, mine);
       cut(a, static_cast<float>(h.tiles) * static_cast<float>(h.blocks) * a.p.n_kv);
       base[0] = base[1] = base[2] = 0;
-      total = h.tiles * a.p.n_kv * pieces(h.blocks);
+      const int units = h.tiles * a.p.n_kv;
+      total = units * pieces(h.blocks);
+      if (uneven(a, total, total - units)) {
+        Tries t{};
+        count(a, h, t);
+        fit(a, t);
+        total = units * pieces(h.blocks);
+      }
       return;
     }
     const int s0 = threadIdx.x * per, s1 = min(s0 + per, a.p.n_seqs);
@@ -247,17 +312,28 @@ struct Plan {
       n += static_cast<float>(h.tiles) * static_cast<float>(h.blocks) * a.p.n_kv;
     }
     cut(a, block_sum<NT>(n, reinterpret_cast<float*>(lds)));
-    int v[3] = {0, 0, 0}, tot[3];
-    for (int s = s0; s < s1; ++s) {
-      const Share<ROWS, KEYS> h(a, seq(a, s));
-      const int units = h.tiles * a.p.n_kv, pc = pieces(h.blocks);
-      v[0] += units * pc;
-      v[1] += pc > 1 ? units : 0;
-      v[2] += pc > 1 ? units * pc : 0;
-    }
-    scan3<NT>(v, tot, lds);
+    int tot[3];
+    count_all(a, s0, s1, tot, lds);
+    if (uneven(a, tot[0], tot[2])) {
+      Tries t{};
+      for (int s = s0; s < s1; ++s) count(a, Share<ROWS, KEYS>(a, seq(a, s)), t);
 #pragma unroll
-    for (int i = 0; i < 3; ++i) base[i] = v[i];
+      for (int i = 0; i < 2; ++i) {
+        const int sum = wave_scan(static_cast<int>(fminf(t.items[2 * i], 1023.f)) |
+                                  static_cast<int>(fminf(t.items[2 * i + 1], 1023.f)) << 16);
+        if (threadIdx.x % kWave == kWave - 1) lds[threadIdx.x / kWave * 2 + i] = sum;
+      }
+      __syncthreads();
+      t = Tries{};
+#pragma unroll
+      for (int w = 0; w < NT / kWave * 2; ++w) {
+        t.items[w % 2 * 2] += static_cast<float>(lds[w] & 0xFFFF);
+        t.items[w % 2 * 2 + 1] += static_cast<float>(static_cast<uint32_t>(lds[w]) >> 16);
+      }
+      __syncthreads();
+      fit(a, t);
+      count_all(a, s0, s1, tot, lds);
+    }
     total = tot[0];
   }
 

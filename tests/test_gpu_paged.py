@@ -225,6 +225,17 @@ def test_decode_long(lens, heads, group, d, f8):
     b.check()
 
 
+def test_decode_pieces_fitted_to_rounds():
+    """Cuts that give a few more pieces than run at once, which are made again with longer
+    ones: of one sequence, of ragged ones, of more than a workgroup has threads."""
+    rng = np.random.default_rng(5)
+    for lens, heads, group in (([6500], 10, 1), (rng.integers(900, 4000, 12).tolist(), 8, 2),
+                               (rng.integers(1, 300, 299).tolist() + [20000], 2, 1)):
+        b = Batch(lens, kv_heads=heads, group=group, d=64, page=32)
+        b.attend()
+        b.check()
+
+
 def test_decode_more_items_than_workgroups():
     rng = np.random.default_rng(3)
     b = Batch(rng.integers(0, 90, 700).tolist(), kv_heads=8, group=2, d=64)
@@ -323,6 +334,14 @@ def test_chunk_window(window, page):
 @pytest.mark.parametrize("heads,group,d,f8", [(1, 1, 64, False), (2, 4, 128, False), (1, 8, 128, True)])
 def test_chunk_long(lens, new, heads, group, d, f8):
     b = Batch(lens, new, kv_heads=heads, group=group, d=d, page=64, f8=f8, act="bf16" if f8 else "f16")
+    b.attend()
+    b.check(rounded=True)
+
+
+@pytest.mark.parametrize("lens,new,group", [([3000, 1200, 2000], [250, 256, 200], 4),
+                                            ([3100, 1300, 2000, 900, 2300], [60, 64, 33, 41, 50], 1)])
+def test_chunk_pieces_fitted_to_rounds(lens, new, group):
+    b = Batch(lens, new, kv_heads=8, group=group, d=64, page=32)
     b.attend()
     b.check(rounded=True)
 
