@@ -235,8 +235,8 @@ struct Plan {
   // ``target`` items run at once, so X times the rounds of them is about the time: X times 5/4, 3/2 or
   // 2 is taken where its pieces fit into so many fewer rounds (16 sequences of 2056-4099 positions,
   // 8 heads of one or two tiles 59.5 -> 54 us, 12 ragged ones 45.2 -> 37.8, three chunks of 256 tokens
-  // 136 -> 117). The counts are estimates: quotients are rounded, and a thread's share ends
-  // at 1023 (ten bits, so that a wave's sum has 16). The cut stays the lengths' alone.
+  // 136 -> 117). The counts are estimates (quotients are rounded); of at most 4 * target items
+  // at X, and fewer at more, two counts' sums fit into a word. The cut stays the lengths' alone.
   __device__ __forceinline__ int longer(int i) const {  // less than 2^31: X is at most 10^9
     return i == 0 ? most : (i == 1 ? most + most / 4 : (i == 2 ? most + most / 2 : 2 * most));
   }
@@ -319,8 +319,7 @@ struct Plan {
       for (int s = s0; s < s1; ++s) count(a, Share<ROWS, KEYS>(a, seq(a, s)), t);
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        const int sum = wave_scan(static_cast<int>(fminf(t.items[2 * i], 1023.f)) |
-                                  static_cast<int>(fminf(t.items[2 * i + 1], 1023.f)) << 16);
+        const int sum = wave_scan(static_cast<int>(t.items[2 * i]) | static_cast<int>(t.items[2 * i + 1]) << 16);
         if (threadIdx.x % kWave == kWave - 1) lds[threadIdx.x / kWave * 2 + i] = sum;
       }
       __syncthreads();
