@@ -397,6 +397,29 @@ def test_chunk_values_that_later_tokens_bring(value, new, d, act):
         assert torch.equal(b.out[:-1], c.out[:-1])
 
 
+@pytest.mark.parametrize("new", [1, 5, 40, 200])
+@pytest.mark.parametrize("f8", [False, True])
+def test_sequences_that_share_pages(new, f8):
+    """A common beginning in pages that two sequences name."""
+    b = Batch([700, 650, 300], [new, new, 1], kv_heads=2, group=2, d=128, page=16, f8=f8)
+    b.table[1, :20] = b.table[0, :20]
+    b.table[2, :3] = b.table[0, :3]
+    b.attend()
+    b.check(rounded=True)
+
+
+@pytest.mark.parametrize("new", [1, 5, 40, 300])
+@pytest.mark.parametrize("d,act", [(128, "f16"), (64, "bf16")])
+def test_values_and_queries_that_are_not_finite(new, d, act):
+    """A visible infinity stays in its element, a NaN query in its head's row."""
+    b = Batch([900, 400], [new, new], kv_heads=2, group=2, d=d, act=act)
+    at = b.at(0, 130, 1)
+    b.slots(b.v_pool)[at[0], at[1], 1, 7] = math.inf
+    b.q[new, d + 3] = math.nan
+    b.attend()
+    b.check(rounded=True)
+
+
 def test_chunk_of_one_token_each_equals_decode():
     a = Batch([100, 0, 1, 4000], kv_heads=2, group=4, d=128)
     b = Batch([100, 0, 1, 4000], [1, 1, 1, 1], kv_heads=2, group=4, d=128)
