@@ -255,9 +255,10 @@ pg::Pool pool_of(const vt_paged_kv& kv) {
 // know of a batch is on the device): 16 (attn_rows_kernel), 64 or 128 (attn_chunk_kernel).
 // All take every batch; keys and values pass once per tile and a tile's rows cost the
 // same whether they are there or not. Measured with 16 / 64 / 128 (us), rows per sequence:
-// 16 sequences of 4096 positions, 8 heads: 16 rows 55 / 63 / 74, 32 rows 62 / 65 / 75, 64 rows 96 /
-// 65 / 76, 128 rows 164 / 88 / 78; with 8-bit caches 29 / 54 / 62, 35 / 53 / 61, 58 / 54 / 62, 107 / 85 / 67;
-// one of 32768: 32 rows 32 / 42 / 56, 64 rows 48 / 43 / 57; one prompt of 4096 rows 617 / 239 / 182.
+// 16 sequences of 4096 positions, 8 heads: 16 rows 54 / 60 / 70, 32 rows 61 / 63 / 71, 64 rows 97 /
+// 63 / 72, 128 rows 168 / 87 / 75; with 8-bit caches 29 / 53 / 61, 36 / 53 / 59, 58 / 53 / 61, 110 / 87 / 64;
+// one of 32768: 32 rows 32 / 41 / 54, 64 rows 49 / 42 / 55, 128 rows 83 / 50 / 56 (a single long one
+// is the exception: the host does not know lengths).
 int tile_rows(const vt_paged_kv& kv, const vt_paged_io& io) {
   if (!io.q_begin) return 16;
   const double rows = static_cast<double>(io.n_tok) * (io.n_q_heads / kv.n_kv_heads) / kv.n_seqs;

@@ -425,9 +425,9 @@ inline int64_t grid_of(const AttnArgs& a, int rows) {
 
 // Work items aimed at by the largest tiles, two workgroups of which a compute unit holds.
 // The smaller tiles aim at half of that, one per compute unit: their pieces wait for
-// memory, and longer ones have less to start, to end and to join (64 sequences of 2000-4097
-// positions, 8 heads: 157 us with 512, 151 with 256; one of 131071 with 8-bit numbers 62
-// and 56; 512 rows per head over 33280 positions on the largest tiles 791 and 1144).
+// memory, and longer ones have less to start, to end and to join (one sequence of 131071
+// positions with 8-bit numbers: 61 us with 512, 57 with 256; 64 of 8 tokens 136 and 110;
+// 512 rows per head over 33280 positions on the largest tiles 583 and 737).
 constexpr int kTarget = 512;
 constexpr size_t kSyncBytes = 8192;   // the counters, at the start of the workspace
 static_assert(kTarget * 4 <= kSyncBytes, "");
