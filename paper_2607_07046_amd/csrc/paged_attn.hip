@@ -12,11 +12,10 @@
 // each of its 8 keys (16 lanes have a row, 256 bytes) and turns its 8 x 8 numbers in
 // registers, so neither K nor V passes through LDS.
 //
-// The weights are exp2(s - ref), ref a row's reference that follows its maximum only
-// when that rises by more than 8 (weights up to 2^8 keep their relative precision), so
-// sums and outputs are hardly ever rescaled. A weight enters the product as its rounding
-// and the rounding of the remainder (two products; the matrix cores have the time):
-// the output's error is then that of its own rounding.
+// The weights are exp2(s - ref), ref a row's reference that follows its maximum seldom (kLag,
+// kTop). A weight enters the product as its rounding and the rounding of the remainder (two
+// products; the matrix cores have the time): the output's error is then that of its own
+// rounding, and for fp16 up to 2^-32 of the largest value per key that the wave takes.
 //
 // What bounds it: every key and value is read once per tile, from HBM. A wave loads
 // the next 32 keys and values (16 KiB) while it works on these. Measured: 64 sequences of
@@ -247,10 +246,10 @@ __global__ void __launch_bounds__(RT, 2) attn_rows_kernel(AttnArgs a) {
     float top = y[0];
 #pragma unroll
     for (int e = 1; e < 8; ++e) top = fmaxf(top, y[e]);
-    if (__builtin_amdgcn_ballot_w64(top > ref + 8.f) != 0) {
+    if (__builtin_amdgcn_ballot_w64(top > ref + (T::kTop + kLag)) != 0) {
       top = fmaxf(top, __shfl_xor(top, 16, kWave));
       top = fmaxf(top, __shfl_xor(top, 32, kWave));
-      const float next = fmaxf(top, ref);
+      const float next = fmaxf(top - T::kTop, ref);
       const float alpha = next == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ref - next);
       ref = next;
       sum *= alpha;
@@ -260,16 +259,18 @@ __global__ void __launch_bounds__(RT, 2) attn_rows_kernel(AttnArgs a) {
         for (int r = 0; r < 4; ++r) o[m][r] *= alpha;
     }
     const float base = ref == -INFINITY ? 0.f : ref;
+    float all = 0.f;  // of this step: small weights together before they join a sum that may be large
     u32x4 hi, lo;
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
       const float pa = __builtin_amdgcn_exp2f(y[2 * w] - base), pb = __builtin_amdgcn_exp2f(y[2 * w + 1] - base);
-      sum += pa + pb;
+      all += pa + pb;
       hi[w] = T::pack2(pa, pb);
       float ra, rb;
       T::unpack2(hi[w], ra, rb);
       lo[w] = T::pack2(pa - ra, pb - rb);
     }
+    sum += all;
     // V's operands: element m of the lane's 8 keys. Words w of keys 2 i, 2 i + 1 hold
     // elements 2 w, 2 w + 1 (8-bit: 4 w .. 4 w + 3)
     u32x4 vf[NM];

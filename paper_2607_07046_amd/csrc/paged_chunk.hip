@@ -14,9 +14,9 @@
 // whose fragments take one chunk of 32 rows, and at c ^ 2 (r % (CPR / 2)) for V, whose
 // transposing reads take two chunks of four rows.
 //
-// Weights are exp2(s - ref), ref a row's reference that follows the maximum when that
-// rises by more than 8, so sums and outputs are seldom rescaled; they enter the
-// product rounded once, as much as the output itself is.
+// Weights are exp2(s - ref), ref a row's reference that follows the maximum seldom (kLag, kTop);
+// they enter the product rounded once, as much as the output itself is (for fp16 also off by up to
+// 2^-32 of the largest value per key).
 //
 // What bounds it: the products, 4 D flops per row and key, whose matrix instructions share a SIMD
 // with as many cycles of exponentials, packing and LDS reads, and the card's power (the
@@ -335,7 +335,7 @@ __global__ void __launch_bounds__(CTH, 2) attn_chunk_kernel(AttnArgs a) {
   // a new reference for the rows: the largest score so far
   auto refer = [&](float top) {
     top = fmaxf(top, __shfl_xor(top, 32, kWave));
-    const float next = fmaxf(top, ref);
+    const float next = fmaxf(top - T::kTop, ref);
     const float alpha = next == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ref - next);
     ref = next;
     sum *= alpha;
@@ -344,16 +344,19 @@ __global__ void __launch_bounds__(CTH, 2) attn_chunk_kernel(AttnArgs a) {
 #pragma unroll
       for (int i = 0; i < 16; ++i) o[m][i] *= alpha;
   };
-  // scores to weights, the second product's operand, and their sum
+  // scores to weights, the second product's operand, and their sum (a block's together before they
+  // join a sum that may be large)
   auto weigh = [&](const f32x16& s, u32x4 (&pf)[2], float& sum) {
     const float base = ref == -INFINITY ? 0.f : ref;
+    float all = 0.f;
 #pragma unroll
     for (int w = 0; w < 8; ++w) {
       const float pa = __builtin_amdgcn_exp2f(fmaf(s[2 * w], sc, -base));
       const float pb = __builtin_amdgcn_exp2f(fmaf(s[2 * w + 1], sc, -base));
-      sum += pa + pb;
+      all += pa + pb;
       pf[w / 4][w % 4] = T::pack2(pa, pb);
     }
+    sum += all;
   };
   // Bits of keys lo .. hi - 1 of the block of 32 from key p0 on.
   auto span = [](int p0, int lo, int hi) {
@@ -513,7 +516,7 @@ __global__ void __launch_bounds__(CTH, 2) attn_chunk_kernel(AttnArgs a) {
             __builtin_amdgcn_sched_barrier(0);
           }
           wa.end(pa, suma);
-          const bool raise_a = __builtin_amdgcn_ballot_w64(topa * sc > ref + 8.f) != 0;
+          const bool raise_a = __builtin_amdgcn_ballot_w64(topa * sc > ref + (T::kTop + kLag)) != 0;
           asm volatile("" : "+v"(pa[0]), "+v"(pa[1]), "+v"(suma));
           if (raise_a) break;
           sum += suma;
@@ -529,7 +532,7 @@ __global__ void __launch_bounds__(CTH, 2) attn_chunk_kernel(AttnArgs a) {
             __builtin_amdgcn_sched_barrier(0);
           }
           wb.end(pb, sumb);
-          const bool raise_b = __builtin_amdgcn_ballot_w64(topb * sc > ref + 8.f) != 0;
+          const bool raise_b = __builtin_amdgcn_ballot_w64(topb * sc > ref + (T::kTop + kLag)) != 0;
           asm volatile("" : "+v"(pb[0]), "+v"(pb[1]), "+v"(sumb));
           if (raise_b) {
             ++t;  // A is done
@@ -560,7 +563,7 @@ __global__ void __launch_bounds__(CTH, 2) attn_chunk_kernel(AttnArgs a) {
           f32x16 s = f32x16{};
 #pragma unroll
           for (int c = 0; c < NK; ++c) s = T::mfma32(kf[c], qf[c], s);
-          if (__builtin_amdgcn_ballot_w64(largest(s) > ref + 8.f) != 0) break;
+          if (__builtin_amdgcn_ballot_w64(largest(s) > ref + (T::kTop + kLag)) != 0) break;
           weigh(s, pf, sum);
 #pragma unroll
           for (int m = 0; m < NM; ++m)
