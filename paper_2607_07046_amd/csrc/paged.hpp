@@ -67,7 +67,10 @@ struct BFloat {
                                                    0, 0);
   }
   static constexpr uint32_t kExp = 0x7F807F80u;
-  static constexpr float kTop = 0.f;
+  // Weights up to 2^-32: fewer than 2^31 of them with values up to 2^128 add up to less than 2^127, so sums of
+  // finite values are finite (with weights around 1 values of 3e38 gave infinity). Weights down to 2^-126
+  // are still 2^-86 of the maximum's.
+  static constexpr float kTop = -40.f;
 };
 
 // Whether either half of a word is an infinity or NaN of type T.

@@ -60,3 +60,20 @@ def test_many_small_weights_beside_one_large(new, act, f8, d):
     assert bool(((got - want).abs() <= tol).all()), float((got - want).abs().max())
     lse = b.lse.double().view(count, t, 8)
     assert bool(((lse - total.log()[:, None]).abs() <= 2.0 ** -12 + 2.0 ** -18 + (d + 8) * 2.0 ** -24 * 18).all())
+
+
+@pytest.mark.parametrize("new", FORMS)
+@pytest.mark.parametrize("size", [3e38, 1e30, 1e-20])
+def test_values_near_the_largest_numbers(new, size):
+    """Values alike at every position give themselves, whatever the weights: also where sums of
+    them are beyond fp32."""
+    lens = [max(n, new or 1) for n in (1, 2, 40, 900, 20000)]
+    b = Batch(lens, [new] * 5 if new else None, kv_heads=2, group=2, d=64, act="bf16", page=64)
+    value = (torch.linspace(0.5, 1.0, 64, device="cuda") * size).bfloat16()
+    value[1::2] *= -1
+    for s, n in enumerate(b.lens):
+        b.slots(b.v_pool)[b.at(s)] = value
+    b.attend()
+    got, want = b.out.double().view(-1, 64), value.double()
+    # the output's rounding, one of each weight and of their sum, fp32 sums
+    assert bool(((got - want).abs() <= (3 * half_step(b.dtype) + 2.0 ** -15) * want.abs()).all())
