@@ -17,7 +17,8 @@ constexpr float kF8Max = 448.f;
 
 // Weights of a softmax are exp2(score - ref), ref a row's reference, 2^kTop below its maximum when it is
 // set and following that when it rises by more than kLag: weights end at 2^(kTop + kLag), so sums and
-// outputs are hardly ever rescaled.
+// outputs are hardly ever rescaled. What is compared with kTop + kLag is a weight's own exponent as the weight
+// takes it: beside scores whose steps are larger than kLag no other rounding bounds it.
 constexpr float kLag = 8.f;
 
 // The activations' 16-bit type. pack2 rounds to nearest even.

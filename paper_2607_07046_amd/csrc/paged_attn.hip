@@ -202,6 +202,7 @@ __global__ void __launch_bounds__(RT, 2) attn_rows_kernel(AttnArgs a) {
     }
   };
   auto work = [&](int i, Tile<F8, D>& x) {
+#pragma clang fp contract(off)  // weights are those of the rounded scores, as the reference is
     const int p0 = start(i);
     f32x4 s[2];
 #pragma unroll
@@ -246,7 +247,7 @@ __global__ void __launch_bounds__(RT, 2) attn_rows_kernel(AttnArgs a) {
     float top = y[0];
 #pragma unroll
     for (int e = 1; e < 8; ++e) top = fmaxf(top, y[e]);
-    if (__builtin_amdgcn_ballot_w64(top > ref + (T::kTop + kLag)) != 0) {
+    if (__builtin_amdgcn_ballot_w64(top - ref > T::kTop + kLag) != 0) {
       top = fmaxf(top, __shfl_xor(top, 16, kWave));
       top = fmaxf(top, __shfl_xor(top, 32, kWave));
       const float next = fmaxf(top - T::kTop, ref);

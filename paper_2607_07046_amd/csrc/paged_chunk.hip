@@ -325,12 +325,12 @@ __global__ void __launch_bounds__(CTH, 2) attn_chunk_kernel(AttnArgs a) {
     }
     return f;
   };
-  // the largest of a lane's scores, in units of the weights' exponents
+  // the largest of a lane's scores
   auto largest = [&](const f32x16& s) {
     float top = s[0];
 #pragma unroll
     for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
-    return top * sc;
+    return top;
   };
   // a new reference for the rows: the largest score so far
   auto refer = [&](float top) {
@@ -344,9 +344,9 @@ __global__ void __launch_bounds__(CTH, 2) attn_chunk_kernel(AttnArgs a) {
 #pragma unroll
       for (int i = 0; i < 16; ++i) o[m][i] *= alpha;
   };
-  // scores to weights, the second product's operand, and their sum (a block's together before they
-  // join a sum that may be large)
-  auto weigh = [&](const f32x16& s, u32x4 (&pf)[2], float& sum) {
+  // scores (times sc the weights' exponents) to weights, the second product's operand, and their sum (a
+  // block's together before they join a sum that may be large)
+  auto weigh = [&](const f32x16& s, float sc, u32x4 (&pf)[2], float& sum) {
     const float base = ref == -INFINITY ? 0.f : ref;
     float all = 0.f;
 #pragma unroll
@@ -389,8 +389,15 @@ __global__ void __launch_bounds__(CTH, 2) attn_chunk_kernel(AttnArgs a) {
         sync_or(a.p.status, VT_PAGED_BAD_PAGE);
       used = own16(span(p0, any_lo, any_hi) & ~gone);
     }
+    {
+      // rounded before the reference is taken from them: where a score's step is larger than the
+      // weights' range, the reference's rounding must be the weights'
+#pragma clang fp contract(off)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[i] = s[i] * sc;
+    }
     refer(largest(s));
-    weigh(s, pf, sum);
+    weigh(s, 1.f, pf, sum);
     // values that no row of the wave sees stay out of the product even if they are
     // infinite
     auto seen = [&](int m, int b, uint32_t keys) {  // a fragment's values of these of the lane's keys
@@ -516,7 +523,7 @@ __global__ void __launch_bounds__(CTH, 2) attn_chunk_kernel(AttnArgs a) {
             __builtin_amdgcn_sched_barrier(0);
           }
           wa.end(pa, suma);
-          const bool raise_a = __builtin_amdgcn_ballot_w64(topa * sc > ref + (T::kTop + kLag)) != 0;
+          const bool raise_a = __builtin_amdgcn_ballot_w64(fmaf(topa, sc, -ref) > T::kTop + kLag) != 0;
           asm volatile("" : "+v"(pa[0]), "+v"(pa[1]), "+v"(suma));
           if (raise_a) break;
           sum += suma;
@@ -532,7 +539,7 @@ __global__ void __launch_bounds__(CTH, 2) attn_chunk_kernel(AttnArgs a) {
             __builtin_amdgcn_sched_barrier(0);
           }
           wb.end(pb, sumb);
-          const bool raise_b = __builtin_amdgcn_ballot_w64(topb * sc > ref + (T::kTop + kLag)) != 0;
+          const bool raise_b = __builtin_amdgcn_ballot_w64(fmaf(topb, sc, -ref) > T::kTop + kLag) != 0;
           asm volatile("" : "+v"(pb[0]), "+v"(pb[1]), "+v"(sumb));
           if (raise_b) {
             ++t;  // A is done
@@ -563,8 +570,8 @@ __global__ void __launch_bounds__(CTH, 2) attn_chunk_kernel(AttnArgs a) {
           f32x16 s = f32x16{};
 #pragma unroll
           for (int c = 0; c < NK; ++c) s = T::mfma32(kf[c], qf[c], s);
-          if (__builtin_amdgcn_ballot_w64(largest(s) > ref + (T::kTop + kLag)) != 0) break;
-          weigh(s, pf, sum);
+          if (__builtin_amdgcn_ballot_w64(fmaf(largest(s), sc, -ref) > T::kTop + kLag) != 0) break;
+          weigh(s, sc, pf, sum);
 #pragma unroll
           for (int m = 0; m < NM; ++m)
 #pragma unroll

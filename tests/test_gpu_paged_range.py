@@ -77,3 +77,40 @@ def test_values_near_the_largest_numbers(new, size):
     got, want = b.out.double().view(-1, 64), value.double()
     # the output's rounding, one of each weight and of their sum, fp32 sums
     assert bool(((got - want).abs() <= (3 * half_step(b.dtype) + 2.0 ** -15) * want.abs()).all())
+
+
+@pytest.mark.parametrize("new", FORMS)
+@pytest.mark.parametrize("act,sigma", [("f16", 300.0), ("f16", 5000.0), ("f16", 20000.0), ("bf16", 1e6), ("bf16", 1e12)])
+def test_scores_far_beyond_their_rounding(new, act, sigma):
+    """Scores of 10^5 to 10^24, whose fp32 steps are larger than the weights' range: the weights are
+    those of the rounded scores, finite, and one key that stands out by more than the scores' errors
+    takes all. (``check`` derives the scores' error and asserts that all is finite where the definition is.)"""
+    lens = [max(n, new or 1) for n in (1, 33, 700, 5000)]
+    b = Batch(lens, [new] * 4 if new else None, kv_heads=2, group=2, d=128, act=act, page=32, sigma=0.0)
+    g, most = torch.Generator(device="cuda").manual_seed(3), 60000.0 if act == "f16" else 1e30
+    big = lambda *shape: torch.empty(shape, device="cuda").normal_(0, sigma, generator=g).clamp(-most, most)
+    for s, n in enumerate(b.lens):
+        b.slots(b.k_pool)[b.at(s)] = big(n, 2, 128).to(b.dtype)
+    b.q[:b.rows] = big(b.rows, b.nq * 128).to(b.dtype)
+    b.attend()
+    b.check(rounded=True)
+    # where the largest score stands out, its value (rounded, with its weight and the sum's rounding)
+    row, clear = 0, 0
+    for s, (n, t) in enumerate(zip(b.lens, b.new)):
+        k, v = b.read(b.k_pool, s), b.read(b.v_pool, s)
+        q = b.q[row:row + t].double().view(t, 2, 2, 128).permute(1, 2, 0, 3).reshape(2, 2 * t, 128)
+        kt = k.permute(1, 2, 0).contiguous()
+        x = torch.matmul(q, kt) / math.sqrt(128)
+        hidden = torch.arange(n, device="cuda") > torch.arange(n - t, n, device="cuda").repeat(2)[:, None]
+        e = 2 * 132 * 2.0 ** -24 * torch.matmul(q.abs(), kt.abs()).amax(-1) / math.sqrt(128) + 40
+        best = x.masked_fill(hidden, -math.inf).topk(min(2, n), -1)
+        alone = best.values[..., 0] - best.values[..., -1] > e if n > 1 else torch.ones_like(e, dtype=torch.bool)
+        alone |= ~best.values[..., -1].isfinite()
+        at = best.indices[..., 0]
+        want = v.permute(1, 0, 2).gather(1, at[..., None].expand(-1, -1, 128))
+        got = b.out[row:row + t].double().view(t, 2, 2, 128).permute(1, 2, 0, 3).reshape(2, 2 * t, 128)
+        off = (got - want).abs() - 3 * half_step(b.dtype) * want.abs() - 2.0 ** -20
+        assert bool((off[alone] <= 0).all()), (s, float(off[alone].max()))
+        clear += int(alone.sum())
+        row += t
+    assert clear > b.rows  # of 4 heads: the test tests something
