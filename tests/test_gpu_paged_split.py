@@ -1,5 +1,5 @@
-"""Splits of a paged batch at their limits, on the device: the most pieces that a call comes to, and
-chunks of more sequences than a workgroup has threads."""
+"""Splits of a paged batch at their limits, on the device: the most pieces that a call comes to, chunks
+of more sequences than a workgroup has threads, replays of a captured chunk."""
 import numpy as np
 import pytest
 import torch
@@ -44,3 +44,31 @@ def test_chunks_of_many_sequences(most, mean_rows, f8, window):
     b.attend()
     b.check(rounded=True)
     assert int(b.status) == 0
+
+
+@pytest.mark.parametrize("pad,rows", [(4, 16), (60, 64), (500, 128)])
+def test_replays_of_a_chunk_follow_lengths_and_rows(pad, rows):
+    """One captured call serves other lengths, rows and tables, idle slots and padding among them; with eager
+    work in between. (The host chose the tile when it captured.)"""
+    b = Batch([900, 40, 3000, 17], [40, 9, 7, 4], kv_heads=2, group=2, d=128, page=16, pad=pad)
+    assert tile_rows([b.n_tok, 0, 0, 0], 2) == rows
+    ws = b.workspace()
+    b.attend(ws)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        b.attend(ws, sync=False)
+    full = list(b.lens)
+    for lens, new in ((full, [40, 9, 7, 4]), ([900, 0, 2999, 5], [1, 0, 58, 1]), ([0, 0, 0, 0], [0, 0, 0, 0]),
+                      ([60, 40, 1000, 17], [60, 0, 0, 0]), (full, [1, 1, 1, 1])):
+        b.lens, b.new, b.rows = lens, new, sum(new)
+        b.len.copy_(torch.tensor(lens, dtype=torch.int32))
+        b.begin.copy_(torch.tensor([0] + new).cumsum(0).to(torch.int32))
+        b.q[:b.rows] = torch.randn((b.rows, b.q.shape[1]), device="cuda").to(b.dtype)
+        torch.randn(300, 300, device="cuda").sum()
+        for _ in range(2):
+            b.out.fill_(7.0)
+            b.lse.fill_(7.0)
+            g.replay()
+            torch.cuda.synchronize()
+            assert not ws[:8192].any()
+            b.check(rounded=True)
