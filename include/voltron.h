@@ -518,9 +518,10 @@ vt_status vt_layer_decode_emit(const vt_shard_spec* spec, const vt_layer_weights
  *
  * Everything that changes from step to step (lengths, table, new tokens per
  * sequence) is device memory that the kernels read, so one captured graph
- * serves every step. What they hold is checked there: a page outside the
- * pool is never touched (its keys are not stored, or count as masked), and the
- * status word says so. */
+ * serves every step. Pages and lengths are checked there: a page outside the
+ * pool is never touched, nor is the table read past its end (such keys are not
+ * stored, or count as masked), and the status word says so. q_begin is not checked: it
+ * must ascend. */
 
 /* Number formats of activations and of a paged cache. VT_T_F8E4M3 is the OCP
  * 8-bit float (4 exponent, 3 mantissa bits, largest 448, no infinities); as a
@@ -543,7 +544,9 @@ enum { VT_T_F16 = 0, VT_T_BF16 = 1, VT_T_F8E4M3 = 2 };
  * Table entries past a sequence's last position are not read. Sequences may
  * share pages that none of them writes. table, len, the scales and status need
  * 4-byte alignment only. Up to 65536 sequences of fewer than 2^31 - 4095
- * positions. */
+ * positions. (Every workgroup of an attention call looks at all lengths: up to some
+ * 1000 sequences that hardly shows, 4096 short ones take two and a half times as long per
+ * sequence, 65536 forty times.) */
 typedef struct vt_paged_kv {
   void* k;
   void* v;
@@ -634,10 +637,13 @@ vt_status vt_paged_decode_attn(const vt_paged_kv* kv, const vt_paged_io* io, flo
 
 /* The same for a chunk of new tokens per sequence (io->q_begin; NULL as
  * above): the token at position p attends to positions 0..p, the last
- * ``window`` of them if window > 0. Chunks of any lengths may be mixed. Where
- * the batch has more than 32 rows (new tokens x query heads per KV head) per
- * sequence, the weights enter the product with the values rounded once to the
- * activations' type. */
+ * ``window`` of them if window > 0. Chunks of any lengths may be mixed, but one
+ * kind of kernel takes the whole batch, chosen by the host's only measure of it, the
+ * mean of its rows per sequence, n_tok x query heads per KV head / n_seqs, padding
+ * rows and idle slots counted. Where that is more than 32, the weights enter the product
+ * with the values rounded once to the activations' type, for every sequence of the batch;
+ * up to 32 as above. The roundings of a sequence's results, and their speed, thus depend on the
+ * sequences beside it: a prompt among many single tokens is faster in a call of its own. */
 vt_status vt_paged_chunk_attn(const vt_paged_kv* kv, const vt_paged_io* io, float scale,
                               int32_t window, void* ws, size_t ws_bytes, void* stream);
 

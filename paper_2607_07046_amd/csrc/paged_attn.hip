@@ -19,11 +19,11 @@
 //
 // What bounds it: every key and value is read once per tile, from HBM. A wave loads
 // the next 32 keys and values (16 KiB) while it works on these. Measured: 64 sequences of
-// 2061-4097 positions, 64 query heads on 8 KV heads of 128, fp16: 153 us for 818 MB, 5.3 TB/s (HBM
-// reads by the counters 819 MB, matrix cores busy 5%); 125 ragged ones of up to 2053, 32 heads, bf16: 418
-// us for 2.29 GB, 5.5 TB/s; one of 131071, 8-bit: 55 us for 268 MB, 4.9 TB/s. A 4 GiB device
-// copy moves 4.7 TB/s. For short ones the chain lengths -> split -> page -> keys -> join
-// bounds it: one sequence of 129 positions 5.8 us in a captured graph, of 4096 11.1.
+// 2061-4097 positions, 64 query heads on 8 KV heads of 128, fp16: 151-153 us for 818 MB, 5.4 TB/s (HBM
+// reads by the counters 819 MB, matrix cores busy 5%); 125 ragged ones of up to 2053, 32 heads, bf16: 418-430
+// us for 2.29 GB, 5.3-5.5 TB/s; one of 131071, 8-bit: 55-57 us for 268 MB, 4.7-4.9 TB/s. A 4 GiB device
+// copy moves 4.7-4.9 TB/s. For short ones the chain lengths -> split -> page -> keys -> join
+// bounds it: one sequence of 129 positions 5.9 us in a captured graph, of 4096 11.1.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>

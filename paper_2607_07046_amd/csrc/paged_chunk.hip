@@ -18,14 +18,18 @@
 // they enter the product rounded once, as much as the output itself is (for fp16 also off by up to
 // 2^-32 of the largest value per key).
 //
-// What bounds it: the products, 4 D flops per row and key, whose matrix instructions share a SIMD
-// with as many cycles of exponentials, packing and LDS reads, and the card's power (the
-// clock falls from 2.5 to 1.9-2.1 GHz). Measured: a prompt of 8192 tokens, 32 query heads on 8, bf16: 558
-// us, 985 TFLOP/s (products of 8192^3 by the library in the same loop 1086-1156); one of
-// 4096, 32 heads, fp16 173-187 us, 735-795; 512 tokens per head behind 32768 positions with
-// 8-bit numbers 575-600 us, 925-965; matrix cores busy 36-41% of the cycles. Whole blocks of keys
-// take an inner loop without masks, in which one block's weights stand between another's products;
-// with the masks inside 617 and 196 us for the first two.
+// What bounds it: no one pipe. A stage is 1024 cycles of matrix instructions for a wave and about as many
+// of vector ones (exponentials, packing), and a SIMD has two waves; for a prompt of 4096 tokens the two
+// take about 5300 cycles for their stages, more than both pipes' work in a row. A's scores
+// and B's product stand alone in their wave, the two waves keep no phase, and a third of the LDS's busy cycles
+// are bank conflicts. Measured (LDS conflicts / active, matrix cores busy): that prompt, 32 heads, fp16, 173-187 us,
+// 735-795 TFLOP/s (0.32, 36%); ragged prompts of up to 1999 with a window of 1024, group 4, 163-172 us (0.32, 30%); 512
+// tokens per head behind 32768 positions with 8-bit numbers 572-600 us, 925-970 (0.39, 40%); a prompt of
+// 8192, 32 query heads on 8, bf16, 558-569 us, 967-985 (the library's products of 8192^3 of such numbers 1280-1380).
+// The clock falls from 2.5 to 2.0-2.1 GHz.
+// Whole blocks of keys take an inner loop without masks, in which one block's weights stand between another's
+// products; with the masks inside 617 and 196 us for prompts of 8192 and 4096 tokens. At head size 128 the 8-bit
+// kernels keep 17-40 registers, and the 16-bit ones with pages below 16 positions 12-19, in scratch.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
