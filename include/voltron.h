@@ -626,7 +626,8 @@ vt_status vt_paged_workspace_size(const vt_paged_kv* kv, const vt_paged_io* io, 
  * weights enter the product with the values as two numbers of the activations'
  * type, their rounding and its remainder. With VT_T_F16 a weight may besides be off by
  * 2^-32 of its row's largest one: over n positions out by up to n 2^-32 of the largest
- * value (2^-15 at 131072), lse not at all. A query that sees no key (an idle
+ * value (2^-15 at 131072), lse not at all. With VT_T_BF16 sums of the largest finite
+ * values do not overflow, and values below 2^-86 (10^-26) may count as zero. A query that sees no key (an idle
  * slot) gets out 0 and lse -infinity. Values and keys outside the visible
  * positions, and of bad pages, have no influence whatever they hold; a visible
  * value that is infinite or NaN leaves its element of the output infinite or
