@@ -648,6 +648,141 @@ vt_status vt_paged_decode_attn(const vt_paged_kv* kv, const vt_paged_io* io, flo
 vt_status vt_paged_chunk_attn(const vt_paged_kv* kv, const vt_paged_io* io, float scale,
                               int32_t window, void* ws, size_t ws_bytes, void* stream);
 
+/* ---- The rest of a batch's layer (paper Sec. 2.1: RMSNorm, the linear projections, rotary
+ * positions and the gated FFN around the attention; Sec. 3.2.1: on a shard's rows and columns) ----
+ * With the paged cache above, one step of a shard for the tokens of many sequences (a row each) is
+ *   vt_norm_rows            x (+ partial + peer) -> h, normalised
+ *   vt_linear               Q, K and V in one product (weights stacked), with their bias
+ *   vt_paged_append_heads   per-head norms, rotation, keys and values into their pages
+ *   vt_paged_decode_attn / vt_paged_chunk_attn
+ *   vt_linear               output projection: the partial sum, or added to the residual
+ *   vt_norm_rows, vt_linear_gated, vt_linear    the FFN
+ * Numbers are VT_T_F16 or VT_T_BF16, one type for all operands of a call; sums, norms and
+ * angles are fp32 or more, and each result is rounded once. Matrices are [rows][ld]: a row's numbers
+ * from its length up to the next multiple of 8 may be read (whatever they hold, they change nothing) and
+ * are never written. Infinities and NaN in a row or a weight reach the results as in the formulas. Everything
+ * but the descriptors is device memory of the current device, and ``stream`` is one of that device. Up to 2^20
+ * rows a call. */
+
+/* Activation functions: z, max(z, 0), z / (1 + exp(-z)), z Phi(z) with the normal distribution's
+ * Phi, and its approximation z (1 + tanh(sqrt(2 / pi) (z + 0.044715 z^3))) / 2. VT_ACT_RELU of NaN is 0. */
+enum { VT_ACT_NONE = 0, VT_ACT_RELU = 1, VT_ACT_SILU = 2, VT_ACT_GELU = 3, VT_ACT_GELU_TANH = 4 };
+
+/* A projection of rows. */
+typedef struct vt_linear_io {
+  int32_t type;
+  int32_t act;             /* VT_ACT_* */
+  int32_t n_rows;
+  int32_t n_in;
+  int32_t n_out;
+  const void* x;           /* [n_rows][ld_x >= n_in], ld_x up to 2^22 */
+  int64_t ld_x;
+  const void* w;           /* [n_out][ld_w >= n_in], ld_w up to 2^22 */
+  int64_t ld_w;
+  const void* bias;        /* nullable: [n_out] */
+  const void* w_up;        /* vt_linear_gated only: as w */
+  int64_t ld_up;
+  const void* bias_up;     /* vt_linear_gated only, nullable: [n_out] */
+  const void* residual;    /* nullable: [n_rows][ld_res >= n_out]; may be y itself (same ld) */
+  int64_t ld_res;
+  void* y;                 /* out: [n_rows][ld_y >= n_out]; overlaps nothing else */
+  int64_t ld_y;
+} vt_linear_io;
+
+/* Bytes of device workspace that vt_linear and vt_linear_gated need (64 MiB and 16 KiB, the
+ * same for every shape). It must be zero-filled once before its first use by these two entry points (it
+ * is theirs alone); they leave its synchronisation words zero after every call. One
+ * workspace must not be used by two calls that may run at the same time (captured graphs that share one
+ * included). */
+vt_status vt_linear_workspace_size(const vt_linear_io* io, size_t* bytes);
+
+/* y = act(x w^T + bias) + residual, in one launch. A row's result does not depend on the rows
+ * beside it but for the order of its fp32 sums, which n_rows, n_in and n_out decide; equal calls give equal
+ * bits. */
+vt_status vt_linear(const vt_linear_io* io, void* ws, size_t ws_bytes, void* stream);
+
+/* y = act(x w^T + bias) * (x w_up^T + bias_up) + residual: both projections of a gated feed-forward
+ * block, its activation and the product, in one launch. */
+vt_status vt_linear_gated(const vt_linear_io* io, void* ws, size_t ws_bytes, void* stream);
+
+/* Rows to normalise. */
+typedef struct vt_norm_io {
+  int32_t type;
+  int32_t n_rows;
+  int32_t hidden;          /* up to 16384 */
+  float eps;               /* finite, >= 0 */
+  const void* x;           /* [n_rows][ld_x >= hidden] */
+  int64_t ld_x;
+  const void* partial;     /* nullable, as x: this device's partial sum */
+  int64_t ld_partial;
+  const void* peer;        /* nullable, as x: the sum of the other devices' */
+  int64_t ld_peer;
+  const void* gain;        /* [hidden] */
+  void* h;                 /* out, nullable: [n_rows][ld_h >= hidden]; may be x, partial or peer (same ld) */
+  int64_t ld_h;
+  void* y;                 /* out: [n_rows][ld_y >= hidden]; may be x, partial or peer (same ld), not h */
+  int64_t ld_y;
+} vt_norm_io;
+
+/* h = x + partial + peer, rounded, and y = h / sqrt(mean(h^2) + eps) * gain of h as rounded (h NULL:
+ * the same without writing it). Squares of finite numbers do not overflow. */
+vt_status vt_norm_rows(const vt_norm_io* io, void* stream);
+
+/* Rotary positions. Pair i of a head's first ``dims`` numbers (i and i + dims / 2 with
+ * VT_ROPE_HALVES, else 2i and 2i + 1; the others stay) turns by pos * f_i and grows by ``amplitude``,
+ *   f_i = base^(-2i/dims) (k + (1 - k) / factor):
+ * a context stretched by ``factor`` slows the pairs down that turn fewer than ``low`` times (k = 0)
+ * within ``context`` positions, leaves those alone that turn more than ``high`` times (k = 1), and goes
+ * linearly in their number of turns between. low = high = 0 slows all of them down. Angles are reduced in
+ * double. */
+typedef struct vt_rope {
+  int32_t dims;            /* even, up to head_dim; 0: the whole head */
+  uint32_t flags;          /* VT_ROPE_HALVES or 0 */
+  float base;              /* 0: no rotation */
+  float factor;            /* >= 1; 0 stands for 1 */
+  float low;
+  float high;              /* above low, or both 0 */
+  int32_t context;         /* >= 1 with low or high */
+  float amplitude;         /* > 0; 0 stands for 1 */
+} vt_rope;
+
+/* Norms per head, before the rotation: x / sqrt(mean(x^2) + eps) * gain over the head's numbers. */
+typedef struct vt_head_norm {
+  const void* q_gain;      /* nullable (queries as they are): [head_dim], for all query heads */
+  const void* k_gain;      /* nullable (keys as they are): [head_dim], for all key heads */
+  float eps;               /* finite, >= 0 */
+} vt_head_norm;
+
+/* vt_paged_append with norms per head and any rotation above, in the same pass: ``norm`` and
+ * ``rope`` may be NULL (none). Nothing is rounded between norm and rotation. Values are stored as they come. All
+ * else (rows that are skipped, bad pages, the status word, 8-bit caches) as vt_paged_append. */
+vt_status vt_paged_append_heads(const vt_paged_kv* kv, const vt_paged_io* io, const vt_head_norm* norm,
+                                const vt_rope* rope, void* stream);
+
+/* Rows of query and key heads without a cache (for vt_kv_append, which stores keys as they come, or a
+ * cache of the caller's). */
+typedef struct vt_heads_io {
+  int32_t type;
+  int32_t n_tok;
+  int32_t head_dim;        /* 64 or 128 */
+  const int32_t* pos;      /* device [n_tok], 4-byte aligned; NULL: row r is at pos0 + r. Rows at a negative
+                              position are skipped: nothing is written for them */
+  int32_t pos0;
+  int32_t n_q_heads;       /* up to 1024; 0: none */
+  const void* q;           /* [n_tok][ld_q >= n_q_heads * head_dim] */
+  int64_t ld_q;
+  void* q_out;             /* as q; may be q (same ld) */
+  int64_t ld_qo;
+  int32_t n_k_heads;       /* the same for the keys */
+  const void* k;
+  int64_t ld_k;
+  void* k_out;
+  int64_t ld_ko;
+} vt_heads_io;
+
+/* q_out and k_out = queries and keys with their norms and rotated, as above. */
+vt_status vt_rotate_heads(const vt_heads_io* io, const vt_head_norm* norm, const vt_rope* rope, void* stream);
+
 /* Static text of a status code. */
 const char* vt_status_string(vt_status s);
 

@@ -1,0 +1,150 @@
+// Shared by the kernels of vt_linear and vt_linear_gated: arguments and epilogue.
+#pragma once
+
+#include "device.hpp"
+#include "internal.hpp"
+#include "paged.hpp"
+
+namespace vt {
+namespace lin {
+
+using pg::BFloat;
+using pg::Half;
+
+constexpr float kLog2e = 1.4426950408889634f;
+
+// y = act(x W^T + bias) + residual, gated: act(x W^T + bias) * (x W_up^T + bias_up) + residual.
+struct Args {
+  const uint16_t* x;
+  const uint16_t* w[2];
+  const uint16_t* bias[2];
+  const uint16_t* res;
+  uint16_t* y;
+  int64_t ld_x, ld_w[2], ld_r, ld_y;
+  int32_t M, N, K, act;
+  int32_t m_tiles, n_tiles;
+  int32_t splits, steps;  // slices of K, and the k-steps of each
+  float* part;            // the slices' sums
+  uint32_t* arrived;      // per tile: slices done, zero between calls
+};
+
+// The workspace: arrival counters, then the slices' sums.
+constexpr int kMaxTiles = 4096;  // of a split product
+constexpr size_t kSyncBytes = kMaxTiles * sizeof(uint32_t);
+constexpr size_t kPartBytes = size_t(64) << 20;
+
+// The activation functions in fp32. Half a step of the results' type is 2^-12 at least; exp2 and
+// the reciprocal are the hardware's, a few 2^-24 off.
+__device__ __forceinline__ float sigmoid(float z) {
+  return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-kLog2e * z));
+}
+
+// z Phi(z) with Phi(z) = erfc(-z / sqrt 2) / 2. erfc(x) = exp(-x^2) t Q(t), t = 1 / (1 + 0.54 x): the
+// coefficients of Q are a fit to the scaled function over x >= 0 of least largest relative error (3.1e-6), so
+// the left tail keeps its relative precision, which 1 + erf loses.
+__device__ __forceinline__ float gelu(float z) {
+  const float t = __builtin_amdgcn_rcpf(fmaf(0.54f * 0.70710678f, fabsf(z), 1.f));
+  float q = 0.097615257f;
+  q = fmaf(q, t, -0.31480265f);
+  q = fmaf(q, t, 0.21606381f);
+  q = fmaf(q, t, 0.12524414f);
+  q = fmaf(q, t, 0.26698509f);
+  q = fmaf(q, t, 0.30422452f);
+  q = fmaf(q, t, 0.30467153f);
+  const float h = 0.5f * t * q * __builtin_amdgcn_exp2f(-0.5f * kLog2e * z * z);
+  return z * (z > 0.f ? 1.f - h : h);
+}
+
+// W values through the activation (uniform).
+template <int W>
+__device__ __forceinline__ void activate(float (&z)[W], int act) {
+  switch (act) {
+    case VT_ACT_RELU:
+#pragma unroll
+      for (int e = 0; e < W; ++e) z[e] = z[e] > 0.f ? z[e] : 0.f;
+      break;
+    case VT_ACT_SILU:
+#pragma unroll
+      for (int e = 0; e < W; ++e) z[e] *= sigmoid(z[e]);
+      break;
+    case VT_ACT_GELU:
+#pragma unroll
+      for (int e = 0; e < W; ++e) z[e] = gelu(z[e]);
+      break;
+    case VT_ACT_GELU_TANH:  // (1 + tanh u) / 2 = sigmoid(2 u)
+#pragma unroll
+      for (int e = 0; e < W; ++e)
+        z[e] *= sigmoid(1.5957691216057308f * z[e] * fmaf(0.044715f * z[e], z[e], 1.f));
+      break;
+    default: break;
+  }
+}
+
+template <class T>
+__device__ __forceinline__ float one(const uint16_t* p) {
+  float a, b;
+  T::unpack2(*p, a, b);
+  return a;
+}
+
+// W (4 or 8) consecutive features n.. of row m, from the product's sums to y. Whole groups by wide
+// accesses; the group that reaches past N by single numbers, so no byte outside is read or written
+// but a row's own.
+template <class T, bool GATED, int W>
+__device__ __forceinline__ void finish(const Args& a, int m, int n, float (&z)[W], float (&u)[W]) {
+  typedef unsigned int vec __attribute__((ext_vector_type(W / 2)));
+  const bool whole = n + W <= a.N;
+  auto add = [&](const uint16_t* p, float (&to)[W]) {
+    if (whole) {
+      const vec v = *reinterpret_cast<const vec*>(p);
+#pragma unroll
+      for (int e = 0; e < W / 2; ++e) {
+        float lo, hi;
+        T::unpack2(v[e], lo, hi);
+        to[2 * e] += lo;
+        to[2 * e + 1] += hi;
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < W; ++e)
+        if (n + e < a.N) to[e] += one<T>(p + e);
+    }
+  };
+  if (a.bias[0]) add(a.bias[0] + n, z);
+  activate(z, a.act);
+  if (GATED) {
+    if (a.bias[1]) add(a.bias[1] + n, u);
+#pragma unroll
+    for (int e = 0; e < W; ++e) z[e] *= u[e];
+  }
+  if (a.res) add(a.res + m * a.ld_r + n, z);
+  uint16_t* y = a.y + m * a.ld_y + n;
+  vec v;
+#pragma unroll
+  for (int e = 0; e < W / 2; ++e) v[e] = T::pack2(z[2 * e], z[2 * e + 1]);
+  if (whole) {
+    *reinterpret_cast<vec*>(y) = v;
+  } else {
+#pragma unroll
+    for (int e = 0; e < W; ++e)
+      if (n + e < a.N) y[e] = static_cast<uint16_t>(v[e / 2] >> (16 * (e % 2)));
+  }
+}
+
+// The 8 numbers of w with those at index >= v set to zero.
+__device__ __forceinline__ u32x4 keep_first(u32x4 w, int v) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) w[i] = v >= 2 * i + 2 ? w[i] : (v == 2 * i + 1 ? (w[i] & 0xFFFFu) : 0u);
+  return w;
+}
+
+// 16 bytes at a lane's offset plus a uniform one. Only the lane's is range-checked: it is kOOB where
+// nothing is to be read.
+__device__ __forceinline__ u32x4 load_at(rsrc_t r, uint32_t lane_off, uint32_t off) {
+  return __builtin_amdgcn_raw_buffer_load_b128(r, lane_off, off, 0);
+}
+
+hipError_t launch_thin(const Args& a, bool bf16, bool gated, int mb, int ob, hipStream_t s);
+
+}  // namespace lin
+}  // namespace vt

@@ -12,12 +12,6 @@ namespace pg {
 
 constexpr int CT = 256;  // threads per workgroup
 
-// Frequencies of the rotated pairs in revolutions per position, in double: at
-// position 10^6 a float's angle would be off by 0.06 rad.
-struct Freq {
-  double rev[64];
-};
-
 struct AppendArgs {
   Pool p;
   const uint16_t* q;
@@ -28,40 +22,6 @@ struct AppendArgs {
   const int32_t* q_begin;
   int32_t n_tok, n_q;
 };
-
-// The sequence whose rows end after row r: the number of ends q_begin[1..] that are
-// <= r, found by all lanes of a wave 64 probes at a time (two round trips up to
-// 4096 sequences).
-__device__ __forceinline__ int sequence_of(const int32_t* q_begin, int n, int r) {
-  const int lane = threadIdx.x % kWave;
-  int lo = 0;
-  while (n > kWave) {
-    const int step = (n + kWave - 1) / kWave, i = (lane + 1) * step - 1;
-    const bool below = i < n && q_begin[lo + i + 1] <= r;
-    const int whole = __builtin_popcountll(__builtin_amdgcn_ballot_w64(below));
-    lo += whole * step;
-    n = min(step, n - whole * step);
-  }
-  const bool below = lane < n && q_begin[lo + lane + 1] <= r;
-  return lo + __builtin_popcountll(__builtin_amdgcn_ballot_w64(below));
-}
-
-// Eight numbers as e4m3: value / scale rounded to nearest even, saturating; NaN stays.
-__device__ __forceinline__ u32x2 to_f8(const float (&x)[8], float scale) {
-  float y[8];
-#pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    const float t = x[e] / scale;
-    y[e] = t > kF8Max ? kF8Max : (t < -kF8Max ? -kF8Max : t);
-  }
-  u32x2 r;
-#pragma unroll
-  for (int w = 0; w < 2; ++w) {
-    int t = __builtin_amdgcn_cvt_pk_fp8_f32(y[4 * w], y[4 * w + 1], 0, false);
-    r[w] = __builtin_amdgcn_cvt_pk_fp8_f32(y[4 * w + 2], y[4 * w + 3], t, true);
-  }
-  return r;
-}
 
 // A workgroup takes one token: a thread turns the same 8 elements (with HALVES two
 // groups of 8, half a head apart) of several heads, so their cosines and sines are
@@ -76,24 +36,9 @@ __global__ void __launch_bounds__(CT) append_kernel(AppendArgs a, Freq f) {
   const int c = threadIdx.x % CPR, hl = threadIdx.x / CPR;
   const int r = blockIdx.x, nkv = a.p.n_kv, rows = 2 * nkv + (a.q ? a.n_q : 0);
   const int first = blockIdx.y * HL + hl, step = gridDim.y * HL;
-  int s = r;
-  int64_t pos;
-  if (a.q_begin) {
-    s = __builtin_amdgcn_readfirstlane(sequence_of(a.q_begin, a.p.n_seqs, r));
-    if (s >= a.p.n_seqs) return;  // behind the last sequence
-    pos = static_cast<int64_t>(a.p.len[s]) - a.q_begin[s + 1] + r;
-  } else {
-    pos = static_cast<int64_t>(a.p.len[s]) - 1;
-  }
-  if (pos < 0 || pos > INT32_MAX) return;
-  uint32_t bad = pos >= a.p.capacity ? VT_PAGED_BAD_LEN : 0u;
-  int page = 0;
-  if (!bad) {
-    page = a.p.table[s * a.p.ld_table + (pos >> a.p.shift)];
-    if (page < 0 || page >= a.p.n_pages) bad = VT_PAGED_BAD_PAGE;
-  }
-  if (bad && a.p.status && threadIdx.x == 0 && blockIdx.y == 0) sync_or(a.p.status, bad);
-  const int64_t at = static_cast<int64_t>(bad ? 0 : page) * a.p.page + (pos & a.p.mask) * a.p.slot;
+  int64_t pos, at;
+  bool bad;
+  if (!place_row(a.p, a.q_begin, r, threadIdx.x == 0 && blockIdx.y == 0, pos, at, bad)) return;
 
   float cs[NP], sn[NP];
 #pragma unroll
@@ -159,7 +104,10 @@ namespace {
 
 constexpr int kMaxHeads = 1024, kMaxTokens = 1 << 20, kMaxSeqs = 1 << 16;
 
-bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+}  // namespace
+
+namespace vt {
+namespace pg {
 
 vt_status check_paged(const vt_paged_kv* kv, const vt_paged_io* io) {
   if (!kv || !io) return fail(VT_ERR_ARG, "null cache or io");
@@ -224,11 +172,11 @@ vt_status check_rows(const void* p, int64_t ld, int64_t n, const char* name) {
   return VT_OK;
 }
 
-pg::Pool pool_of(const vt_paged_kv& kv) {
+Pool pool_of(const vt_paged_kv& kv) {
   const int64_t elem = kv.type == VT_T_F8E4M3 ? 1 : 2;
   int shift = 0;
   while ((1 << shift) < kv.page_size) ++shift;
-  pg::Pool p{};
+  Pool p{};
   p.k = static_cast<char*>(kv.k);
   p.v = static_cast<char*>(kv.v);
   p.page = kv.page_stride * elem;
@@ -245,11 +193,18 @@ pg::Pool pool_of(const vt_paged_kv& kv) {
   p.shift = shift;
   p.mask = kv.page_size - 1;
   p.capacity = static_cast<int32_t>(
-      std::min<int64_t>(static_cast<int64_t>(kv.max_pages) * kv.page_size, pg::kMaxPositions));
+      std::min<int64_t>(static_cast<int64_t>(kv.max_pages) * kv.page_size, kMaxPositions));
   p.n_kv = kv.n_kv_heads;
   p.n_seqs = kv.n_seqs;
   return p;
 }
+
+}  // namespace pg
+}  // namespace vt
+
+namespace {
+
+using namespace vt::pg;
 
 // Rows of an attention tile, by the mean rows of a sequence (what else the host could
 // know of a batch is on the device): 16 (attn_rows_kernel), 64 or 128 (attn_chunk_kernel).

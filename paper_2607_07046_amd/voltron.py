@@ -31,6 +31,7 @@ VT_W_INT8, VT_W_INT4 = 1, 2
 VT_T_F16, VT_T_BF16, VT_T_F8E4M3 = 0, 1, 2
 VT_PAGED_BAD_PAGE, VT_PAGED_BAD_LEN = 1, 2
 VT_ROPE_HALVES = 1
+VT_ACT_NONE, VT_ACT_RELU, VT_ACT_SILU, VT_ACT_GELU, VT_ACT_GELU_TANH = 0, 1, 2, 3, 4
 VT_WS_ERROR_WORD = 8192  # byte offset of the workspace's barrier error word
 VT_NOALLOC_SCRATCH_BYTES = 4 << 20  # the scratch array of vt_layer_decode_noalloc
 
@@ -42,7 +43,8 @@ EXPORTS = ("vt_shard_spec_create", "vt_shard_spec_query", "vt_shard_spec_destroy
            "vt_shard_pack", "vt_kv_copy_heads", "vt_moe_workspace_size", "vt_moe_ffn_decode",
            "vt_stack_decode", "vt_layer_decode_noalloc", "vt_layer_decode_emit",
            "vt_paged_append", "vt_paged_workspace_size", "vt_paged_decode_attn",
-           "vt_paged_chunk_attn")
+           "vt_paged_chunk_attn", "vt_linear_workspace_size", "vt_linear", "vt_linear_gated",
+           "vt_norm_rows", "vt_paged_append_heads", "vt_rotate_heads")
 
 
 class VoltronError(RuntimeError):
@@ -142,6 +144,48 @@ class vt_paged_io(ctypes.Structure):
                 ("out", ctypes.c_void_p), ("ld_out", ctypes.c_int64), ("lse", ctypes.c_void_p)]
 
 
+class vt_linear_io(ctypes.Structure):
+    _fields_ = [("type", ctypes.c_int32), ("act", ctypes.c_int32), ("n_rows", ctypes.c_int32),
+                ("n_in", ctypes.c_int32), ("n_out", ctypes.c_int32),
+                ("x", ctypes.c_void_p), ("ld_x", ctypes.c_int64),
+                ("w", ctypes.c_void_p), ("ld_w", ctypes.c_int64), ("bias", ctypes.c_void_p),
+                ("w_up", ctypes.c_void_p), ("ld_up", ctypes.c_int64),
+                ("bias_up", ctypes.c_void_p),
+                ("residual", ctypes.c_void_p), ("ld_res", ctypes.c_int64),
+                ("y", ctypes.c_void_p), ("ld_y", ctypes.c_int64)]
+
+
+class vt_norm_io(ctypes.Structure):
+    _fields_ = [("type", ctypes.c_int32), ("n_rows", ctypes.c_int32), ("hidden", ctypes.c_int32),
+                ("eps", ctypes.c_float),
+                ("x", ctypes.c_void_p), ("ld_x", ctypes.c_int64),
+                ("partial", ctypes.c_void_p), ("ld_partial", ctypes.c_int64),
+                ("peer", ctypes.c_void_p), ("ld_peer", ctypes.c_int64),
+                ("gain", ctypes.c_void_p),
+                ("h", ctypes.c_void_p), ("ld_h", ctypes.c_int64),
+                ("y", ctypes.c_void_p), ("ld_y", ctypes.c_int64)]
+
+
+class vt_rope(ctypes.Structure):
+    _fields_ = [("dims", ctypes.c_int32), ("flags", ctypes.c_uint32), ("base", ctypes.c_float),
+                ("factor", ctypes.c_float), ("low", ctypes.c_float), ("high", ctypes.c_float),
+                ("context", ctypes.c_int32), ("amplitude", ctypes.c_float)]
+
+
+class vt_head_norm(ctypes.Structure):
+    _fields_ = [("q_gain", ctypes.c_void_p), ("k_gain", ctypes.c_void_p),
+                ("eps", ctypes.c_float)]
+
+
+class vt_heads_io(ctypes.Structure):
+    _fields_ = [("type", ctypes.c_int32), ("n_tok", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("pos", ctypes.c_void_p), ("pos0", ctypes.c_int32),
+                ("n_q_heads", ctypes.c_int32), ("q", ctypes.c_void_p), ("ld_q", ctypes.c_int64),
+                ("q_out", ctypes.c_void_p), ("ld_qo", ctypes.c_int64),
+                ("n_k_heads", ctypes.c_int32), ("k", ctypes.c_void_p), ("ld_k", ctypes.c_int64),
+                ("k_out", ctypes.c_void_p), ("ld_ko", ctypes.c_int64)]
+
+
 class vt_layer_io(ctypes.Structure):
     _fields_ = [("x", ctypes.c_void_p), ("peer_attn", ctypes.c_void_p),
                 ("peer_ffn", ctypes.c_void_p), ("attn_partial", ctypes.c_void_p),
@@ -209,13 +253,23 @@ def load_library(path=None):
     lib.vt_paged_decode_attn.argtypes = [ctypes.POINTER(vt_paged_kv), ctypes.POINTER(vt_paged_io),
                                          ctypes.c_float, I32, P, SZ, P]
     lib.vt_paged_chunk_attn.argtypes = lib.vt_paged_decode_attn.argtypes
+    lib.vt_linear_workspace_size.argtypes = [ctypes.POINTER(vt_linear_io), ctypes.POINTER(SZ)]
+    lib.vt_linear.argtypes = [ctypes.POINTER(vt_linear_io), P, SZ, P]
+    lib.vt_linear_gated.argtypes = lib.vt_linear.argtypes
+    lib.vt_norm_rows.argtypes = [ctypes.POINTER(vt_norm_io), P]
+    lib.vt_paged_append_heads.argtypes = [ctypes.POINTER(vt_paged_kv), ctypes.POINTER(vt_paged_io),
+                                          ctypes.POINTER(vt_head_norm), ctypes.POINTER(vt_rope), P]
+    lib.vt_rotate_heads.argtypes = [ctypes.POINTER(vt_heads_io), ctypes.POINTER(vt_head_norm),
+                                    ctypes.POINTER(vt_rope), P]
     for name in ("vt_shard_spec_create", "vt_shard_spec_query", "vt_kv_append",
                  "vt_workspace_size", "vt_layer_decode", "vt_layer_prefill_chunk",
                  "vt_qplan", "vt_partial_encode", "vt_partial_decode_add",
                  "vt_quantize_rows", "vt_layer_decode_q", "vt_shard_pack", "vt_kv_copy_heads",
                  "vt_moe_workspace_size", "vt_moe_ffn_decode", "vt_stack_decode",
                  "vt_layer_decode_noalloc", "vt_layer_decode_emit", "vt_paged_append",
-                 "vt_paged_workspace_size", "vt_paged_decode_attn", "vt_paged_chunk_attn"):
+                 "vt_paged_workspace_size", "vt_paged_decode_attn", "vt_paged_chunk_attn",
+                 "vt_linear_workspace_size", "vt_linear", "vt_linear_gated", "vt_norm_rows",
+                 "vt_paged_append_heads", "vt_rotate_heads"):
         getattr(lib, name).restype = ctypes.c_int
     lib.vt_status_string.argtypes = [ctypes.c_int]
     lib.vt_status_string.restype = ctypes.c_char_p
@@ -394,3 +448,34 @@ def vt_paged_chunk_attn(kv: vt_paged_kv, io: vt_paged_io, scale, window, ws, ws_
                         stream=None):
     _check(load_library().vt_paged_chunk_attn(ctypes.byref(kv), ctypes.byref(io), scale, window,
                                               ws, ws_bytes, stream))
+
+
+def vt_linear_workspace_size(io: vt_linear_io) -> int:
+    n = ctypes.c_size_t(0)
+    _check(load_library().vt_linear_workspace_size(ctypes.byref(io), ctypes.byref(n)))
+    return n.value
+
+
+def vt_linear(io: vt_linear_io, ws, ws_bytes, stream=None):
+    _check(load_library().vt_linear(ctypes.byref(io), ws, ws_bytes, stream))
+
+
+def vt_linear_gated(io: vt_linear_io, ws, ws_bytes, stream=None):
+    _check(load_library().vt_linear_gated(ctypes.byref(io), ws, ws_bytes, stream))
+
+
+def vt_norm_rows(io: vt_norm_io, stream=None):
+    _check(load_library().vt_norm_rows(ctypes.byref(io), stream))
+
+
+def _ref(struct):
+    return None if struct is None else ctypes.byref(struct)
+
+
+def vt_paged_append_heads(kv: vt_paged_kv, io: vt_paged_io, norm=None, rope=None, stream=None):
+    _check(load_library().vt_paged_append_heads(ctypes.byref(kv), ctypes.byref(io), _ref(norm),
+                                                _ref(rope), stream))
+
+
+def vt_rotate_heads(io: vt_heads_io, norm=None, rope=None, stream=None):
+    _check(load_library().vt_rotate_heads(ctypes.byref(io), _ref(norm), _ref(rope), stream))

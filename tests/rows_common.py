@@ -1,0 +1,145 @@
+"""Rows and weights of a batch on the device, and the definitions in float64.
+
+Matrices have row strides beyond their length; what lies between holds NaN in
+inputs and a mark in outputs.
+"""
+import math
+
+import torch
+
+from paper_2607_07046_amd import voltron as vt
+
+ACT_TYPES = {"f16": (torch.float16, vt.VT_T_F16), "bf16": (torch.bfloat16, vt.VT_T_BF16)}
+ACTS = {"none": vt.VT_ACT_NONE, "relu": vt.VT_ACT_RELU, "silu": vt.VT_ACT_SILU, "gelu": vt.VT_ACT_GELU,
+        "gelu_tanh": vt.VT_ACT_GELU_TANH}
+MARK = 7.0
+
+
+def half_step(dtype):
+    """A rounding's largest relative error."""
+    return torch.finfo(dtype).eps / 2
+
+
+def least(dtype):
+    """A rounding's largest error where numbers have no full precision: half the smallest one."""
+    return float(torch.finfo(dtype).smallest_normal) * torch.finfo(dtype).eps / 2
+
+
+def matrix(g, rows, cols, dtype, pad=8, sigma=1.0, fill=math.nan):
+    """[rows][cols] of a wider buffer whose other numbers are ``fill``."""
+    ld = -(-cols // 8) * 8 + pad
+    t = torch.full((rows, ld), fill, dtype=dtype, device="cuda")
+    t[:, :cols] = torch.empty((rows, cols), device="cuda").normal_(0, sigma, generator=g).to(dtype)
+    return t[:, :cols]
+
+
+def marked(rows, cols, dtype, pad=8):
+    ld = -(-cols // 8) * 8 + pad
+    return torch.full((rows, ld), MARK, dtype=dtype, device="cuda")[:, :cols]
+
+
+def around(t):
+    """The whole buffer of a matrix()."""
+    return torch.as_strided(t, (t.shape[0], t.stride(0)), (t.stride(0), 1))
+
+
+def untouched(t):
+    return bool((around(t)[:, t.shape[1]:] == MARK).all())
+
+
+def p(t):
+    return None if t is None else t.data_ptr()
+
+
+def ld(t):
+    return 0 if t is None else t.stride(0)
+
+
+def stream():
+    return torch.cuda.current_stream().cuda_stream
+
+
+def act64(z, name):
+    if name == "relu":
+        return torch.where(z > 0, z, 0.0)
+    if name == "silu":
+        return z * torch.sigmoid(z)
+    if name == "gelu":
+        return 0.5 * z * torch.special.erfc(-z * math.sqrt(0.5))  # (special.ndtr is 0 below -8)
+    if name == "gelu_tanh":
+        return z * torch.sigmoid(2.0 * math.sqrt(2.0 / math.pi) * (z + 0.044715 * z ** 3))
+    return z
+
+
+class Linear:
+    """One projection: operands on the device, the call, the definition."""
+
+    def __init__(self, type, M, K, N, act="none", bias=False, residual=False, gated=False, pad=8, seed=0, sigma=1.0,
+                 positive=False):
+        g = torch.Generator(device="cuda").manual_seed(seed)
+        self.dtype, self.type = ACT_TYPES[type]
+        self.M, self.K, self.N, self.act, self.gated = M, K, N, act, gated
+        self.x = matrix(g, M, K, self.dtype, pad, sigma)
+        self.w = matrix(g, N, K, self.dtype, pad, K ** -0.5)
+        self.w_up = matrix(g, N, K, self.dtype, pad, K ** -0.5) if gated else None
+        if positive:  # sums that only grow
+            for t in (self.x, self.w):
+                t.abs_()
+        vec = lambda: torch.empty(N, device="cuda").normal_(0, 0.5, generator=g).to(self.dtype)
+        self.bias = vec() if bias else None
+        self.bias_up = vec() if bias and gated else None
+        self.residual = matrix(g, M, N, self.dtype, pad) if residual else None
+        self.y = marked(M, N, self.dtype, pad)
+
+    def io(self, **change):
+        f = dict(type=self.type, act=ACTS[self.act], n_rows=self.M, n_in=self.K, n_out=self.N, x=p(self.x),
+                 ld_x=ld(self.x), w=p(self.w), ld_w=ld(self.w), bias=p(self.bias), w_up=p(self.w_up),
+                 ld_up=ld(self.w_up), bias_up=p(self.bias_up), residual=p(self.residual), ld_res=ld(self.residual),
+                 y=p(self.y), ld_y=ld(self.y))
+        f.update(change)
+        return vt.vt_linear_io(**f)
+
+    def workspace(self):
+        return torch.zeros(vt.vt_linear_workspace_size(self.io()), dtype=torch.uint8, device="cuda")
+
+    def call(self, ws, sync=True, **change):
+        (vt.vt_linear_gated if self.gated else vt.vt_linear)(self.io(**change), ws.data_ptr(), ws.numel(), stream())
+        if sync:
+            torch.cuda.synchronize()
+            assert not ws[:16384].any(), "synchronisation words are not zero after the call"
+        return self.y
+
+    def sums(self, w, bias):
+        """x w^T + bias, and a bound on the error of the fp32 sums. Products are exact. Rounding each of K additions
+        moves a sum by 2^-24 of it at most, and it is at most S = sum |x w|: as independent errors 4 sqrt(K) 2^-24 S
+        is four standard deviations; were a matrix instruction's 32 products cut off and not rounded, all one way,
+        K / 32 times 2^-23 S; 8 more for the slices' sums, the bias and the residual."""
+        x, w = self.x.double(), w.double()
+        b = 0.0 if bias is None else bias.double()
+        e = (4 * math.sqrt(self.K) + self.K / 16 + 8) * 2.0 ** -24
+        return x @ w.t() + b, e * (x.abs() @ w.abs().t() + (0.0 if bias is None else bias.double().abs()))
+
+    def reference(self, residual=None):
+        """The definition, and the bound: the error of the sums through the activation (whose slope is at
+        most 1.13), 2^-16 of the activation itself (its fit is 2^-18 off, exponents are 2^-24 |z| off, |z| below some
+        dozens), and the result's own rounding."""
+        z, ez = self.sums(self.w, self.bias)
+        y = act64(z, self.act)
+        e = 1.13 * ez + (0.0 if self.act in ("none", "relu") else 2.0 ** -16) * y.abs()
+        if self.gated:
+            u, eu = self.sums(self.w_up, self.bias_up)
+            e = e * u.abs() + y.abs() * eu + e * eu
+            y = y * u
+        r = self.residual if residual is None else residual
+        if r is not None:
+            y = y + r.double()
+            e = e + 2.0 ** -23 * (y.abs() + r.double().abs())
+        return y, e + half_step(self.dtype) * (y.abs() + e) + least(self.dtype)
+
+    def check(self, residual=None):
+        want, tol = self.reference(residual)
+        got = self.y.double()
+        off = (got - want).abs() - tol
+        assert bool((off <= 0).all()), (f"worst {float(off.max())} over its tolerance at "
+                                        f"{divmod(int(off.argmax()), off.shape[1])}")
+        assert untouched(self.y), "written outside the rows' numbers"

@@ -1,0 +1,246 @@
+"""vt_linear and vt_linear_gated against float64, element by element."""
+import math
+
+import pytest
+import torch
+
+from paper_2607_07046_amd import voltron as vt
+from tests.rows_common import ACTS, MARK, Linear, act64, around, p
+
+pytestmark = pytest.mark.gpu
+BOTH = pytest.mark.parametrize("type", ["f16", "bf16"])
+
+
+@pytest.fixture(scope="module")
+def ws():
+    return Linear("f16", 1, 8, 8).workspace()
+
+
+# rows, n_in, n_out: single rows and numbers, one less and one more than a tile, a step, a matrix instruction
+SHAPES = [(1, 1, 1), (1, 7, 5), (1, 8, 16), (1, 64, 17), (1, 65, 16), (1, 512, 1536), (1, 4096, 333), (2, 63, 15),
+          (3, 100, 257), (5, 515, 64), (15, 1100, 48), (16, 128, 16), (17, 127, 31), (31, 520, 130), (32, 96, 33),
+          (33, 72, 100), (48, 1000, 77), (63, 65, 129), (64, 512, 512), (65, 640, 63), (100, 2048, 260),
+          (127, 33, 128), (128, 256, 256), (129, 264, 255), (200, 777, 300), (255, 96, 257), (256, 512, 256),
+          (257, 320, 520), (300, 1030, 700), (511, 136, 513), (513, 2050, 264), (1030, 520, 1000)]
+
+
+@BOTH
+@pytest.mark.parametrize("M,K,N", SHAPES)
+def test_shapes(ws, type, M, K, N):
+    x = Linear(type, M, K, N, seed=M + K + N)
+    x.call(ws)
+    x.check()
+
+
+@BOTH
+@pytest.mark.parametrize("M,K,N", SHAPES)
+def test_gated_shapes(ws, type, M, K, N):
+    x = Linear(type, M, K, N, act="silu", gated=True, seed=M + K + N + 1)
+    x.call(ws)
+    x.check()
+
+
+@BOTH
+@pytest.mark.parametrize("act", list(ACTS))
+@pytest.mark.parametrize("gated", [False, True])
+@pytest.mark.parametrize("M", [1, 40, 300])
+def test_epilogue(ws, type, act, gated, M):
+    x = Linear(type, M, 200, 140, act=act, bias=True, residual=True, gated=gated, seed=M, sigma=3.0)
+    x.call(ws)
+    x.check()
+
+
+@BOTH
+@pytest.mark.parametrize("bias,residual", [(True, False), (False, True)])
+@pytest.mark.parametrize("M", [1, 70, 260])
+def test_bias_or_residual(ws, type, bias, residual, M):
+    x = Linear(type, M, 72, 133, bias=bias, residual=residual, seed=3)
+    x.call(ws)
+    x.check()
+
+
+@BOTH
+@pytest.mark.parametrize("M,K,N", [(1, 16384, 64), (4, 8192, 100), (64, 8192, 48), (64, 16000, 260), (130, 8200, 70),
+                                   (200, 9000, 256), (300, 4096, 500)])
+@pytest.mark.parametrize("gated", [False, True])
+def test_long_sums(ws, type, M, K, N, gated):
+    """Few tiles and a long K: slices of K over several workgroups."""
+    x = Linear(type, M, K, N, act="silu" if gated else "none", gated=gated, residual=True, seed=K)
+    x.call(ws)
+    x.check()
+    first = x.y.clone()
+    for _ in range(3):
+        x.y.fill_(MARK)
+        x.call(ws)
+        assert torch.equal(x.y, first), "equal calls, other bits"
+
+
+@BOTH
+def test_growing_sums(ws, type):
+    x = Linear(type, 70, 8192, 96, positive=True, sigma=0.1)
+    x.call(ws)
+    x.check()
+
+
+@BOTH
+@pytest.mark.parametrize("M,K,N", [(1, 512, 96), (1, 9000, 40), (50, 512, 96), (260, 512, 300)])
+def test_residual_in_place(ws, type, M, K, N):
+    x = Linear(type, M, K, N, act="gelu", residual=True, seed=9)
+    before = x.residual.clone()
+    x.call(ws, y=p(x.residual), ld_y=x.residual.stride(0))
+    x.y.copy_(x.residual)
+    x.check(before)
+    assert bool(around(x.residual)[:, N:].isnan().all())
+
+
+@BOTH
+@pytest.mark.parametrize("M", [3, 60, 257, 600])
+@pytest.mark.parametrize("gated", [False, True])
+def test_rows_and_features_apart(ws, type, M, gated):
+    """NaN and infinity in a row or a weight reach its own results and no others."""
+    x = Linear(type, M, 330, 301, gated=gated, act="silu" if gated else "none", seed=5)
+    x.call(ws)
+    clean = x.y.clone()
+    x.x[1, 329] = math.nan
+    x.w[300, 7] = math.inf
+    x.call(ws)
+    rows = torch.arange(M, device="cuda") != 1
+    assert torch.equal(x.y[rows][:, :300], clean[rows][:, :300])
+    assert bool(x.y[1].isnan().all())
+    assert bool((~x.y[:, 300].isfinite()).sum() >= M // 4)  # silu(-inf) * u is NaN, inf stays, and some x are 0
+    assert bool((around(x.y)[:, 301:] == MARK).all())
+
+
+def test_overflow_of_f16(ws):
+    x = Linear("f16", 20, 64, 40, sigma=60000.0)
+    x.x.clamp_(-65504, 65504)
+    x.w.mul_(100)
+    x.call(ws)
+    z, _ = x.sums(x.w, None)
+    big = z.abs() > 66000
+    assert bool((x.y[big].double() == torch.sign(z[big]) * math.inf).all()) and bool(x.y[z.abs() < 65000].isfinite().all())
+
+
+@pytest.mark.parametrize("act", ["silu", "gelu", "gelu_tanh"])
+def test_activations_far_out(ws, act):
+    """x w^T = z exactly, over what bf16 holds: the tails go to 0 and z, never to NaN."""
+    z = torch.cat([torch.linspace(-30, 30, 601), torch.tensor([-3e38, -1e20, -300.0, 300.0, 1e20, 3e38])])
+    x = Linear("bf16", z.numel(), 8, 8, act=act)
+    x.x.zero_()
+    x.w.zero_()
+    x.x[:, 0] = z.cuda().to(torch.bfloat16)
+    x.w[:, 0] = 1.0
+    x.call(ws)
+    exact = x.x[:, 0].double()
+    want = torch.where(exact < -200, 0.0, torch.where(exact > 200, exact, 0.0))
+    mid = exact.abs() <= 200
+    want[mid] = act64(exact[mid], act)
+    got = x.y[:, 0].double()
+    # half a step, the activation's 2^-16, and for tails the exponent's 2^-23 z^2 / 2
+    tol = (2.0 ** -8 + 2.0 ** -16 + 2.0 ** -23 * exact.clamp(-200, 200) ** 2) * want.abs() + 2.0 ** -126
+    assert bool(((got - want).abs() <= tol).all())
+
+
+def test_activations_of_infinities(ws):
+    for act, at_inf in (("none", (math.inf, -math.inf)), ("relu", (math.inf, 0.0)), ("silu", (math.inf, math.nan)),
+                        ("gelu", (math.inf, math.nan)), ("gelu_tanh", (math.inf, math.nan))):
+        x = Linear("f16", 3, 8, 8, act=act, bias=True)
+        x.x.zero_()
+        x.bias[:] = torch.tensor([math.inf, -math.inf, math.nan, 0, 1, -1, 2, -2])
+        x.call(ws)
+        got = x.y[0].double().cpu()
+        for i in range(2):
+            assert math.isnan(got[i]) if math.isnan(at_inf[i]) else got[i] == at_inf[i], (act, i)
+        assert got[2] == 0.0 if act == "relu" else math.isnan(got[2])
+        assert bool(got[3:].isfinite().all())
+
+
+@BOTH
+def test_strides(ws, type):
+    """Rows far apart, as slices of one wide buffer; the widest stride there is."""
+    x = Linear(type, 70, 40, 72, pad=4096, residual=True)
+    x.call(ws)
+    x.check()
+    far = Linear(type, 2, 16, 9, pad=(1 << 22) - 16)
+    assert far.x.stride(0) == 1 << 22
+    far.call(ws)
+    far.check()
+
+
+def test_weights_beyond_2_gib(ws):
+    x = Linear("bf16", 5, 8192, 8)
+    N = 140000
+    w = torch.empty((N, 8192), dtype=torch.bfloat16, device="cuda").normal_(0, 0.01)
+    y = torch.full((5, N), MARK, dtype=torch.bfloat16, device="cuda")
+    x.call(ws, w=p(w), ld_w=8192, n_out=N, y=p(y), ld_y=N)
+    for first in (0, N // 2, N - 300):
+        part = Linear("bf16", 5, 8192, 300)
+        part.x.copy_(x.x)
+        part.w = w[first:first + 300]
+        part.y.copy_(y[:, first:first + 300])
+        part.check()
+
+
+def test_rows_beyond_2_gib(ws):
+    """Outputs, inputs and the residual pass 32-bit offsets."""
+    M, K, N = 70000, 64, 24
+    g = torch.Generator(device="cuda").manual_seed(1)
+    wide = torch.empty((M, 16384), dtype=torch.float16, device="cuda")
+    wide[:, :64].normal_(generator=g)
+    wide[:, 8192:8192 + N].normal_(generator=g)
+    x = Linear("f16", 300, K, N, residual=True)
+    x.call(ws, n_rows=M, x=p(wide), ld_x=16384, residual=wide[:, 8192:].data_ptr(), ld_res=16384,
+           y=wide[:, 12288:].data_ptr(), ld_y=16384)
+    for first in (0, 40000, M - 300):
+        rows = slice(first, first + 300)
+        x.x.copy_(wide[rows, :K])
+        x.residual.copy_(wide[rows, 8192:8192 + N])
+        x.y.copy_(wide[rows, 12288:12288 + N])
+        x.check()
+
+
+def test_two_streams():
+    """Calls at once, each with its workspace."""
+    a, b = Linear("f16", 8, 8192, 64, seed=1), Linear("bf16", 200, 4096, 300, gated=True, act="silu", seed=2)
+    wa, wb = a.workspace(), b.workspace()
+    torch.cuda.synchronize()
+    streams = torch.cuda.Stream(), torch.cuda.Stream()
+    for _ in range(20):
+        for x, w, s in ((a, wa, streams[0]), (b, wb, streams[1])):
+            with torch.cuda.stream(s):
+                x.call(w, sync=False)
+    torch.cuda.synchronize()
+    a.check()
+    b.check()
+
+
+def test_graph_replays(ws):
+    """One captured step of several projections, replayed on new inputs."""
+    xs = [Linear("f16", 1, 4096, 64, seed=1), Linear("f16", 70, 4096, 48, residual=True, seed=2),
+          Linear("f16", 300, 512, 600, gated=True, act="silu", seed=3)]
+    for x in xs:
+        x.call(ws)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        for x in xs:
+            x.call(ws, sync=False)
+    for i in range(4):
+        for x in xs:
+            x.x.copy_(torch.randn(x.x.shape, device="cuda"))
+            x.y.fill_(MARK)
+        graph.replay()
+        torch.cuda.synchronize()
+        for x in xs:
+            x.check()
+        assert not ws[:16384].any()
+
+
+def test_alternating_shapes_share_a_workspace(ws):
+    xs = [Linear("bf16", m, k, n, seed=i, gated=i % 2 == 1) for i, (m, k, n) in
+          enumerate([(1, 8192, 32), (64, 8192, 70), (200, 4096, 128), (2, 300, 4000), (260, 8192, 100)])]
+    for x in xs + xs[::-1]:
+        x.y.fill_(MARK)
+        x.call(ws, sync=False)
+    torch.cuda.synchronize()
+    for x in xs:
+        x.check()
