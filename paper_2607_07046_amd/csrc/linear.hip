@@ -35,12 +35,20 @@ vt_status check_shape(const vt_linear_io* io) {
 }
 
 struct Plan {
-  int mb, ob;  // 16-row and 16-feature blocks of a tile
+  bool tile;   // 256 x 256 tiles
+  int mb, ob;  // else 16-row and 16-feature blocks of a tile
   int m_tiles, n_tiles, splits, steps;
 };
 
 Plan plan_of(int64_t M, int64_t N, int64_t K, bool gated) {
   Plan p{};
+  if (M > 256) {
+    p.tile = true;
+    p.m_tiles = static_cast<int>((M + 255) / 256);
+    p.n_tiles = static_cast<int>(gated ? (N + 127) / 128 : (N + 255) / 256);
+    p.splits = 1;
+    return p;
+  }
   p.mb = M <= 16 ? 1 : (M <= 32 ? 2 : 4);
   p.ob = 1;
   p.m_tiles = static_cast<int>((M + 16 * p.mb - 1) / (16 * p.mb));
@@ -103,7 +111,9 @@ vt_status project(const vt_linear_io* io, bool gated, void* ws, size_t ws_bytes,
   a.part = reinterpret_cast<float*>(static_cast<char*>(ws) + lin::kSyncBytes);
   if ((static_cast<int64_t>(p.n_tiles) * p.splits + 7) / 8 * 8 * p.m_tiles >= (int64_t(1) << 23))  // 2^32 threads
     return fail(VT_ERR_UNSUPPORTED, "%d x %d tiles: fewer rows or features per call", p.m_tiles, p.n_tiles);
-  const hipError_t e = lin::launch_thin(a, io->type == VT_T_BF16, gated, p.mb, p.ob, static_cast<hipStream_t>(stream));
+  const bool bf16 = io->type == VT_T_BF16;
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  const hipError_t e = p.tile ? lin::launch_tile(a, bf16, gated, s) : lin::launch_thin(a, bf16, gated, p.mb, p.ob, s);
   return e == hipSuccess ? VT_OK : fail(VT_ERR_HIP, "projection launch: %s", hipGetErrorString(e));
 }
 

@@ -144,6 +144,7 @@ __device__ __forceinline__ u32x4 load_at(rsrc_t r, uint32_t lane_off, uint32_t o
   return __builtin_amdgcn_raw_buffer_load_b128(r, lane_off, off, 0);
 }
 
+hipError_t launch_tile(const Args& a, bool bf16, bool gated, hipStream_t s);
 hipError_t launch_thin(const Args& a, bool bf16, bool gated, int mb, int ob, hipStream_t s);
 
 }  // namespace lin

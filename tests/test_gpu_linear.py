@@ -21,7 +21,8 @@ SHAPES = [(1, 1, 1), (1, 7, 5), (1, 8, 16), (1, 64, 17), (1, 65, 16), (1, 512, 1
           (3, 100, 257), (5, 515, 64), (15, 1100, 48), (16, 128, 16), (17, 127, 31), (31, 520, 130), (32, 96, 33),
           (33, 72, 100), (48, 1000, 77), (63, 65, 129), (64, 512, 512), (65, 640, 63), (100, 2048, 260),
           (127, 33, 128), (128, 256, 256), (129, 264, 255), (200, 777, 300), (255, 96, 257), (256, 512, 256),
-          (257, 320, 520), (300, 1030, 700), (511, 136, 513), (513, 2050, 264), (1030, 520, 1000)]
+          (257, 320, 520), (300, 1030, 700), (511, 136, 513), (513, 2050, 264), (1030, 520, 1000), (257, 5, 10), (300, 32, 257),
+          (300, 64, 300), (300, 90, 300), (300, 128, 130), (300, 161, 270), (300, 192, 600), (300, 224, 300), (2400, 200, 2500)]
 
 
 @BOTH
