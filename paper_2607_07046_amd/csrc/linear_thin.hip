@@ -12,10 +12,9 @@
 namespace vt {
 namespace lin {
 
-constexpr int KS = 64;  // k of a step
-
-template <class T, bool GATED, int MB, int OB, int NW, int DEPTH>
+template <class T, bool GATED, int MB, int OB, int NW, int HS, int DEPTH>
 __global__ void __launch_bounds__(NW* kWave) thin_kernel(Args a) {
+  constexpr int KS = 32 * HS;  // k of a step
   constexpr int FB = GATED ? 2 * OB : OB, TN = 16 * OB, TM = 16 * MB, LD = 16 * FB + 4, HW = NW / 2;
   __shared__ __attribute__((aligned(16))) float red[HW * TM * LD];
   __shared__ uint32_t ticket;
@@ -29,11 +28,10 @@ __global__ void __launch_bounds__(NW* kWave) thin_kernel(Args a) {
   const int q = lane / 16, r = lane % 16;
 
   const int rows_w = min(TN, a.N - n0), rows_x = min(TM, a.M - m0);
-  rsrc_t rw[2], rx = make_rsrc(a.x + m0 * a.ld_x, static_cast<uint32_t>(rows_x * a.ld_x * 2));
+  const rsrc_t rx = make_rsrc(a.x + m0 * a.ld_x, static_cast<uint32_t>(rows_x * a.ld_x * 2));
+  auto weights = [&](int i) { return make_rsrc(a.w[i] + n0 * a.ld_w[i], static_cast<uint32_t>(rows_w * a.ld_w[i] * 2)); };
+  const rsrc_t rw0 = weights(0), rw1 = GATED ? weights(1) : rw0;
   uint32_t ow[FB], ox[MB];
-#pragma unroll
-  for (int i = 0; i < (GATED ? 2 : 1); ++i)
-    rw[i] = make_rsrc(a.w[i] + n0 * a.ld_w[i], static_cast<uint32_t>(rows_w * a.ld_w[i] * 2));
 #pragma unroll
   for (int b = 0; b < FB; ++b) {
     const int row = 16 * (b % OB) + r;
@@ -50,24 +48,24 @@ __global__ void __launch_bounds__(NW* kWave) thin_kernel(Args a) {
   for (int f = 0; f < FB; ++f)
 #pragma unroll
     for (int b = 0; b < MB; ++b) acc[f][b] = f32x4{0.f, 0.f, 0.f, 0.f};
-  u32x4 wf[DEPTH][FB][2], xf[DEPTH][MB][2];
+  u32x4 wf[DEPTH][FB][HS], xf[DEPTH][MB][HS];
   const int full = a.K / KS, s0 = split * a.steps;
   const int s1 = min(s0 + a.steps, full);
   // step i of this wave; past the slice's end nothing is read and zeros are multiplied
-  auto load = [&](int i, u32x4 (&w)[FB][2], u32x4 (&x)[MB][2]) {
+  auto load = [&](int i, u32x4 (&w)[FB][HS], u32x4 (&x)[MB][HS]) {
     const int s = s0 + wave + i * NW;
     const uint32_t gone = s < s1 ? 0u : kOOB, at = s < s1 ? static_cast<uint32_t>(s * KS * 2) : 0u;
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
+    for (int h = 0; h < HS; ++h) {
 #pragma unroll
-      for (int f = 0; f < FB; ++f) w[f][h] = load_at(rw[f / OB], ow[f] | gone, at + h * 64);
+      for (int f = 0; f < FB; ++f) w[f][h] = load_at(f < OB ? rw0 : rw1, ow[f] | gone, at + h * 64);
 #pragma unroll
       for (int b = 0; b < MB; ++b) x[b][h] = load_at(rx, ox[b] | gone, at + h * 64);
     }
   };
-  auto multiply = [&](const u32x4 (&w)[FB][2], const u32x4 (&x)[MB][2]) {
+  auto multiply = [&](const u32x4 (&w)[FB][HS], const u32x4 (&x)[MB][HS]) {
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
+    for (int h = 0; h < HS; ++h)
 #pragma unroll
       for (int f = 0; f < FB; ++f)
 #pragma unroll
@@ -86,12 +84,12 @@ __global__ void __launch_bounds__(NW* kWave) thin_kernel(Args a) {
   // the step that reaches past K: the numbers behind it are padding and may be anything
   if (a.K % KS != 0 && full >= s0 && full < s0 + a.steps && wave == (full - s0) % NW) {
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
+    for (int h = 0; h < HS; ++h) {
       const int k = full * KS + h * 32 + q * 8;
       const uint32_t gone = k < a.K ? 0u : kOOB;
 #pragma unroll
       for (int f = 0; f < FB; ++f)
-        wf[0][f][h] = keep_first(load_at(rw[f / OB], ow[f] | gone, full * KS * 2 + h * 64), a.K - k);
+        wf[0][f][h] = keep_first(load_at(f < OB ? rw0 : rw1, ow[f] | gone, full * KS * 2 + h * 64), a.K - k);
 #pragma unroll
       for (int b = 0; b < MB; ++b) xf[0][b][h] = keep_first(load_at(rx, ox[b] | gone, full * KS * 2 + h * 64), a.K - k);
     }
@@ -176,9 +174,9 @@ namespace {
 
 template <class T, bool GATED>
 void (*pick(int mb, int ob))(Args) {
-  if (mb == 1) return thin_kernel<T, GATED, 1, 1, 8, 4>;
-  if (mb == 2) return ob == 1 ? thin_kernel<T, GATED, 2, 1, 8, 4> : thin_kernel<T, GATED, 2, 2, 8, 2>;
-  return ob == 1 ? thin_kernel<T, GATED, 4, 1, 8, 2> : thin_kernel<T, GATED, 4, 2, 8, 2>;
+  if (mb == 1) return thin_kernel<T, GATED, 1, 1, 8, 2, 4>;
+  if (mb == 2) return ob == 1 ? thin_kernel<T, GATED, 2, 1, 8, 2, 4> : thin_kernel<T, GATED, 2, 2, 8, 2, 2>;
+  return ob == 1 ? thin_kernel<T, GATED, 4, 1, 8, 2, 2> : thin_kernel<T, GATED, 4, 2, 8, 2, 2>;
 }
 
 }  // namespace
