@@ -1,7 +1,10 @@
 // Loads from memory straight into LDS, and the layout that the projections' kernels give them there.
 //
-// LDS holds blocks of 16 rows x 32 k (1 KiB, one instruction of a wave), chunk c (16 bytes) of row r at unit
-// 4 r + (c ^ (r / 2 % 4) ^ (r / 8)): the rows that one fragment read takes together are in different banks.
+// LDS holds blocks of 8 rows x 64 k (1 KiB): one instruction of a wave, whose 8 lanes of a row read a whole
+// 128-byte line (with 16 rows x 32 k every line was fetched twice, a product of 8192 x 8192 x 8192 took 843 us and
+// not 760). Chunk c (16 bytes) of row r of a fragment of 16 rows is at unit 8 (r % 8) + (c ^ (r / 2)) of block
+// r / 8: the 16 lanes that a fragment's read serves together (0-3, 12-15, 20-23, 24-27 and the like)
+// find it in different banks.
 #pragma once
 
 #include <type_traits>
@@ -11,15 +14,14 @@
 namespace vt {
 namespace lin {
 
-// Row and chunk that lane l's 16 bytes of a block hold, and where its fragment (row l % 16, chunk l / 16) is.
-__device__ __forceinline__ int block_row(int lane) { return lane / 4; }
-__device__ __forceinline__ int block_chunk(int lane) {
-  const int r = lane / 4;
-  return (lane % 4) ^ (r >> 1 & 3) ^ (r >> 3);
-}
+// Row of its block and chunk that lane l's 16 bytes hold; ``half``: which block of a fragment's two it is.
+__device__ __forceinline__ int block_row(int lane) { return lane / 8; }
+__device__ __forceinline__ int block_chunk(int lane, int half) { return (lane % 8) ^ (4 * half + lane / 16); }
+// Where lane l's part of a fragment (row l % 16, chunk l / 16 of the block's k-step) is in the block of its row;
+// the other k-step of 32 is at that address ^ 64.
 __device__ __forceinline__ int fragment_at(int lane) {
   const int r = lane % 16;
-  return (r * 4 + ((lane / 16) ^ (r >> 1 & 3) ^ (r >> 3))) * 16;
+  return (r % 8 * 8 + ((lane / 16) ^ (r / 2))) * 16;
 }
 
 // 16 bytes per lane from r[voff + soff] to LDS at m0 + 16 * lane, in inline asm and waited for by their count: with

@@ -2,7 +2,7 @@
 // linear_thin.hip and linear_tile.hip.
 //
 // WR x WC waves of 16 MBW rows x 16 NBW weight rows each. Both operands come straight into LDS through a
-// ring of ST stages of 32 HS k, up to ST - 1 of them on the way, each number once per tile; the
+// ring of ST stages of 64 HS k, up to ST - 1 of them on the way, each number once per tile; the
 // waves wait for a stage by the count of their own loads and meet once per stage. Two workgroups
 // share a compute unit, so one multiplies while the other waits.
 //
@@ -21,9 +21,10 @@ namespace lin {
 
 template <class T, bool GATED, int WR, int WC, int MBW, int NBW, int HS, int ST>
 __global__ void __launch_bounds__(WR* WC* kWave) mid_kernel(Args a) {
-  constexpr int NW = WR * WC, XU = WR * MBW, WU = WC * NBW, U = HS * (XU + WU), LPS = U / NW;
-  constexpr int NBO = GATED ? NBW / 2 : NBW;  // 16-feature blocks of a wave
-  constexpr int TM = 16 * XU, TN = 16 * WC * NBO, TK = 32 * HS, STAGE = U * 1024, PW = NBO % 2 ? 4 : 8;
+  constexpr int NW = WR * WC, XB = WR * MBW, WB = WC * NBW;  // waves; 16-row blocks of rows and of weights
+  constexpr int UK = 2 * (XB + WB), U = HS * UK, LPS = U / NW;  // units (8 rows x 64 k) of 64 k and of a stage
+  constexpr int NBO = GATED ? NBW / 2 : NBW;                 // 16-feature blocks of a wave
+  constexpr int TM = 16 * XB, TN = 16 * WC * NBO, TK = 64 * HS, STAGE = U * 1024, PW = NBO % 2 ? 4 : 8;
   static_assert(U % NW == 0 && (!GATED || NBW % 2 == 0), "");
   extern __shared__ __attribute__((aligned(16))) char lds[];
   // tiles of the same weights stand on one XCD, one after the other
@@ -37,30 +38,29 @@ __global__ void __launch_bounds__(WR* WC* kWave) mid_kernel(Args a) {
   const bool tail = full * TK < a.K && full >= kt0 && full < kt0 + a.steps;
   const int KT = max(kt1 - kt0, 0) + (tail ? 1 : 0);
 
-  // This wave loads units wave, wave + NW, .. of a stage: unit v is block v % (XU + WU) of its k-step
-  // v / (XU + WU), the rows' blocks first.
+  // This wave loads units wave, wave + NW, .. of a stage: unit v is half v % 2 of block v % UK / 2 of its 64 k
+  // v / UK, the rows' blocks first.
   const int rows_x = min(TM, a.M - m0), rows_w = min(TN, a.N - n0);
   const u32x4 rx = rsrc_words(a.x + m0 * a.ld_x, static_cast<uint32_t>(rows_x * a.ld_x * 2));
   const u32x4 rw0 = rsrc_words(a.w[0] + n0 * a.ld_w[0], static_cast<uint32_t>(rows_w * a.ld_w[0] * 2));
   const u32x4 rw1 = GATED ? rsrc_words(a.w[1] + n0 * a.ld_w[1], static_cast<uint32_t>(rows_w * a.ld_w[1] * 2)) : rw0;
   u32x4 rs[LPS];
   uint32_t off[LPS];
-  const int brow = block_row(lane), bchunk = block_chunk(lane);
 #pragma unroll
   for (int i = 0; i < LPS; ++i) {
-    const int v = wave + NW * i, kh = v / (XU + WU), b = v % (XU + WU);
-    if (b < XU) {
+    const int v = wave + NW * i, b = v % UK / 2, half = v % 2, brow = 8 * half + block_row(lane);
+    if (b < XB) {
       rs[i] = rx;
       off[i] = static_cast<uint32_t>(min(16 * b + brow, rows_x - 1) * a.ld_x * 2);
     } else {
-      const int wb = b - XU, fb = wb % NBW, fo = fb % NBO;
+      const int wb = b - XB, fb = wb % NBW, fo = fb % NBO;
       const bool up = GATED && fb >= NBO;
       const int in = PW == 8 ? 32 * (fo / 2) + 8 * (brow / 4) + 4 * (fo % 2) + brow % 4 : 16 * fo + brow;
       const int row = min(wb / NBW * NBO * 16 + in, rows_w - 1);
       rs[i] = up ? rw1 : rw0;
       off[i] = static_cast<uint32_t>(row * (up ? a.ld_w[1] : a.ld_w[0]) * 2);
     }
-    off[i] += kh * 64 + bchunk * 16;
+    off[i] += v / UK * 128 + block_chunk(lane, half) * 16;
   }
   const uint32_t place0 = lds_address(lds) + wave * 1024;
   int next = kt0, left = kt1 - kt0;
@@ -79,7 +79,7 @@ __global__ void __launch_bounds__(WR* WC* kWave) mid_kernel(Args a) {
     --left;
   };
 
-  const int wr = wave / WC, wc = wave % WC, fa = fragment_at(lane);
+  const int wr = wave / WC, wc = wave % WC, fa = lane % 16 / 8 * 1024 + fragment_at(lane);
   f32x4 acc[NBW][MBW];
 #pragma unroll
   for (int f = 0; f < NBW; ++f)
@@ -88,9 +88,9 @@ __global__ void __launch_bounds__(WR* WC* kWave) mid_kernel(Args a) {
   if (tail) {  // to stage 0, with zeros past K
 #pragma unroll
     for (int i = 0; i < LPS; ++i) {
-      const int k = full * TK + (wave + NW * i) / (XU + WU) * 32 + bchunk * 8;
+      const int u = wave + NW * i, k = full * TK + u / UK * 64 + block_chunk(lane, u % 2) * 8;
       const u32x4 v = load_at(rsrc_of(rs[i]), off[i] | (k < a.K ? 0u : kOOB), full * (TK * 2));
-      *reinterpret_cast<u32x4*>(lds + (wave + NW * i) * 1024 + lane * 16) = keep_first(v, a.K - k);
+      *reinterpret_cast<u32x4*>(lds + u * 1024 + lane * 16) = keep_first(v, a.K - k);
     }
   }
   each<ST - 1>([&](auto Q) {
@@ -105,13 +105,13 @@ __global__ void __launch_bounds__(WR* WC* kWave) mid_kernel(Args a) {
     asm volatile("" ::: "memory");
     load(into);
 #pragma unroll
-    for (int h = 0; h < HS; ++h) {
-      const char* S = lds + cur + h * (XU + WU) * 1024 + fa;
+    for (int h = 0; h < 2 * HS; ++h) {
+      const char* S = lds + cur + h / 2 * UK * 1024 + (fa ^ (h % 2 * 64));
       u32x4 xf[MBW], wf[NBW];
 #pragma unroll
-      for (int b = 0; b < MBW; ++b) xf[b] = *reinterpret_cast<const u32x4*>(S + (wr * MBW + b) * 1024);
+      for (int b = 0; b < MBW; ++b) xf[b] = *reinterpret_cast<const u32x4*>(S + (wr * MBW + b) * 2048);
 #pragma unroll
-      for (int f = 0; f < NBW; ++f) wf[f] = *reinterpret_cast<const u32x4*>(S + (XU + wc * NBW + f) * 1024);
+      for (int f = 0; f < NBW; ++f) wf[f] = *reinterpret_cast<const u32x4*>(S + (XB + wc * NBW + f) * 2048);
 #pragma unroll
       for (int f = 0; f < NBW; ++f)
 #pragma unroll

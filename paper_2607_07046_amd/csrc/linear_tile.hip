@@ -1,9 +1,9 @@
 // Products of many rows: vt_linear and vt_linear_gated on tiles of 256 rows x 256 features.
 //
 // Four waves, one per SIMD, of 128 x 128 each (accumulators in all 256 AGPRs). Both operands go from memory
-// straight into LDS, 16 bytes a lane and 1 KiB an instruction, through a ring of ST stages of 32 k; a wave
-// multiplies one stage while it reads the next one's fragments and sends its share of the loads of one
-// further on, so that nothing stands between two products for longer than the first of them takes. A gated
+// straight into LDS, 16 bytes a lane and 1 KiB an instruction, in k-tiles of 64 through a ring of five half-tiles;
+// a wave multiplies one k-step of 32 while it reads the next one's fragments and sends its share of the loads of a
+// k-tile further on, so that nothing stands between two products for longer than the first of them takes. A gated
 // product's weight blocks are four of the gate and four of the up projection in turn, 64 features of both for each wave, so a
 // feature's two sums are in the same lane.
 //
@@ -21,21 +21,24 @@
 namespace vt {
 namespace lin {
 
-constexpr int TK = 32, TT = 256;
+constexpr int TK = 64, TT = 256;
 constexpr int WALK_M = 8;  // row tiles of a block of an XCD's walk
+constexpr int ST = 5;      // slots of half a k-tile
+constexpr int ER = 64;     // rows of a wave in the epilogue's LDS
 
-// Stages of the ring: as many as one workgroup (the large tiles) or two (128 x 128) have room for.
-constexpr int stages(int mb, int nb) { return mb * nb == 64 ? 5 : (mb * nb == 32 ? 6 : 5); }
-constexpr int stage_bytes(int mb, int nb) { return 2 * (mb + nb) * 1024; }
-constexpr int tile_lds(int mb, int nb) { return stages(mb, nb) * stage_bytes(mb, nb); }
+constexpr int slot_bytes(int mb, int nb) { return 2 * (mb + nb) * 1024; }
+constexpr int tile_lds(int mb, int nb) {
+  const int ring = ST * slot_bytes(mb, nb), epilogue = 4 * ER * (16 * nb + 4) * 4;
+  return ring > epilogue ? ring : epilogue;
+}
 
 // MB, NB: 16-row blocks of rows and of weights of a wave.
 template <class T, bool GATED, int MB, int NB, bool SPLIT>
 __global__ void __launch_bounds__(TT, MB* NB == 16 ? 2 : 1) tile_kernel(Args a) {
   extern __shared__ __attribute__((aligned(16))) char lds[];
-  constexpr int ST = stages(MB, NB), STAGE = stage_bytes(MB, NB), XB = 2 * MB * 1024;
+  constexpr int SLOT = slot_bytes(MB, NB), XB = 2 * MB * 1024;
   constexpr int TM = 32 * MB, TN = 32 * NB, NO = GATED ? TN / 2 : TN;  // rows, weight rows, features of a tile
-  constexpr int P = MB * NB, R = MB + NB, LX = MB / 2, LPS = R / 2;    // products, reads, loads of a wave per k-tile
+  constexpr int P = MB * NB, R = MB + NB, LX = MB / 2, LPS = R / 2;    // products, reads, loads of a wave per half
   // An XCD takes every eighth column of tiles, in blocks of WALK_M rows of them: the tiles that run there
   // at once share rows and weights in its L2.
   const int cols = SPLIT ? a.n_tiles * a.splits : a.n_tiles;
@@ -47,27 +50,31 @@ __global__ void __launch_bounds__(TT, MB* NB == 16 ? 2 : 1) tile_kernel(Args a) 
   const int n_tile = SPLIT ? col % a.n_tiles : col, split = SPLIT ? col / a.n_tiles : 0;
   const int m0 = m_tile * TM, n0 = n_tile * NO;
   const int t = threadIdx.x, lane = t % kWave, wave = __builtin_amdgcn_readfirstlane(t / kWave);
-  const int full = a.K / TK, kt0 = SPLIT ? split * a.steps : 0, kt1 = SPLIT ? min(kt0 + a.steps, full) : full;
+  const int full = a.K / TK, kt0 = SPLIT ? split * a.steps : 0, kt1 = SPLIT ? max(kt0, min(kt0 + a.steps, full)) : full;
   const bool tail = full * TK < a.K && (!SPLIT || (full >= kt0 && full < kt0 + a.steps));
-  const int KT = max(kt1 - kt0, 0) + (tail ? 1 : 0);
 
   const uint32_t lbase = lds_address(lds);
-  // This wave loads a quarter of the rows' blocks and of the weights'; lane l's row and chunk of a
-  // block are what LDS unit l holds.
-  const int brow = block_row(lane), bchunk = block_chunk(lane);
+  // A slot holds the first or the last 8 rows of every 16-row block, 64 k wide; this wave loads a quarter of its
+  // row blocks and of its weight blocks.
+  const int brow = block_row(lane);
   const int which = GATED ? wave % 2 : 0, wrow = (GATED ? wave / 2 : wave) * NB * 8;
   const int rows_x = min(TM, a.M - m0), rows_w = min(NO, a.N - n0);
   u32x4 rx = rsrc_words(a.x + m0 * a.ld_x, static_cast<uint32_t>(rows_x * a.ld_x * 2));
   u32x4 rw = rsrc_words(a.w[which] + n0 * a.ld_w[which], static_cast<uint32_t>(rows_w * a.ld_w[which] * 2));
-  uint32_t xo[LX], wo[NB / 2];
+  uint32_t xo[2][LX], wo[2][NB / 2];
 #pragma unroll
-  for (int u = 0; u < LX; ++u)
-    xo[u] = static_cast<uint32_t>(min(wave * MB * 8 + u * 16 + brow, rows_x - 1) * a.ld_x * 2) + bchunk * 16;
+  for (int h = 0; h < 2; ++h) {
 #pragma unroll
-  for (int u = 0; u < NB / 2; ++u)
-    wo[u] = static_cast<uint32_t>(min(wrow + u * 16 + brow, rows_w - 1) * a.ld_w[which] * 2) + bchunk * 16;
-  // A k-tile's loads of this wave, the rows' first. Past the last k-tile they go on with empty
-  // ranges from offset 0 (no memory traffic, stages that nobody reads), so the counts stay.
+    for (int u = 0; u < LX; ++u)
+      xo[h][u] = static_cast<uint32_t>(min(wave * MB * 8 + u * 16 + h * 8 + brow, rows_x - 1) * a.ld_x * 2) +
+                 block_chunk(lane, h) * 16;
+#pragma unroll
+    for (int u = 0; u < NB / 2; ++u)
+      wo[h][u] = static_cast<uint32_t>(min(wrow + u * 16 + h * 8 + brow, rows_w - 1) * a.ld_w[which] * 2) +
+                 block_chunk(lane, h) * 16;
+  }
+  // A half's loads of this wave, the rows' first. Past the last k-tile they go on with empty
+  // ranges from offset 0 (no memory traffic, slots that nobody reads), so the counts stay.
   uint32_t koff = kt0 * (TK * 2);
   int left = kt1 - kt0;
   const uint32_t placex = lbase + wave * LX * 1024, placew = lbase + XB + wave * (NB / 2) * 1024;
@@ -76,32 +83,35 @@ __global__ void __launch_bounds__(TT, MB* NB == 16 ? 2 : 1) tile_kernel(Args a) 
     constexpr int v = decltype(i)::value;
     return std::integral_constant<int, (v < LX ? v : v - LX) * 1024>{};
   };
-  auto with = [&](auto I, auto&& f) {
-    constexpr int i = decltype(I)::value;
-    if constexpr (i < LX) f(rx, xo[i], koff);
-    else f(rw, wo[i - LX], koff);
+  auto with = [&](auto H, auto I, auto&& f) {
+    constexpr int h = decltype(H)::value, i = decltype(I)::value;
+    if constexpr (i < LX) f(rx, xo[h][i], koff);
+    else f(rw, wo[h][i - LX], koff);
   };
   auto none_left = [&]() {
     rx.z = 0;
     rw.z = 0;
     koff = 0;
   };
-  auto advance = [&]() {
+  auto advance = [&]() {  // after both halves of a k-tile
     koff += TK * 2;
     if (--left <= 0) none_left();
   };
-  auto stage_tail = [&]() {  // the k-tile that reaches past K, with zeros there, to stage 0
+  auto stage_tail = [&]() {  // the k-tile that reaches past K, with zeros there, to the first two slots
     const rsrc_t bx = rsrc_of(rx), bw = rsrc_of(rw);
-    const int k = full * TK + bchunk * 8;
-    const uint32_t gone = k < a.K ? 0u : kOOB;
 #pragma unroll
-    for (int u = 0; u < LX; ++u)
-      *reinterpret_cast<u32x4*>(lds + (wave * LX + u) * 1024 + lane * 16) =
-          keep_first(load_at(bx, xo[u] | gone, full * TK * 2), a.K - k);
+    for (int h = 0; h < 2; ++h) {
+      const int k = full * TK + block_chunk(lane, h) * 8;
+      const uint32_t gone = k < a.K ? 0u : kOOB;
 #pragma unroll
-    for (int u = 0; u < NB / 2; ++u)
-      *reinterpret_cast<u32x4*>(lds + XB + (wave * (NB / 2) + u) * 1024 + lane * 16) =
-          keep_first(load_at(bw, wo[u] | gone, full * TK * 2), a.K - k);
+      for (int u = 0; u < LX; ++u)
+        *reinterpret_cast<u32x4*>(lds + h * SLOT + (wave * LX + u) * 1024 + lane * 16) =
+            keep_first(load_at(bx, xo[h][u] | gone, full * TK * 2), a.K - k);
+#pragma unroll
+      for (int u = 0; u < NB / 2; ++u)
+        *reinterpret_cast<u32x4*>(lds + h * SLOT + XB + (wave * (NB / 2) + u) * 1024 + lane * 16) =
+            keep_first(load_at(bw, wo[h][u] | gone, full * TK * 2), a.K - k);
+    }
   };
 
   const int wm = wave / 2, wn = wave % 2;
@@ -110,65 +120,71 @@ __global__ void __launch_bounds__(TT, MB* NB == 16 ? 2 : 1) tile_kernel(Args a) 
   for (int f = 0; f < NB; ++f)
 #pragma unroll
     for (int b = 0; b < MB; ++b) acc[f][b] = f32x4{0.f, 0.f, 0.f, 0.f};
-  const int xaddr = wm * MB * 1024 + fragment_at(lane), waddr = XB + wn * NB * 1024 + fragment_at(lane);
+  const int fa = fragment_at(lane), xaddr = wm * MB * 1024, waddr = XB + wn * NB * 1024;
+  const bool second = lane % 16 >= 8;  // this lane's row is in a k-tile's second slot
   u32x4 xf[2][MB], wf[2][NB];
-  auto read1 = [&](int i, uint32_t stage, int set) {
-    const char* S = lds + stage;
+  auto read1 = [&](int i, const char* S, int set) {
     if (i < MB) xf[set][i] = *reinterpret_cast<const u32x4*>(S + xaddr + i * 1024);
     else wf[set][i - MB] = *reinterpret_cast<const u32x4*>(S + waddr + (i - MB) * 1024);
   };
-  // The products of a k-tile. In the shadow of their first half the other register set is read (the next
-  // k-tile, from ``stage``), in that of their second half the loads of a later one go out to ``into``.
-  auto multiply = [&](auto SET, uint32_t stage, uint32_t into) {
-    constexpr int set = decltype(SET)::value, H = P / 2;
+  // The products of a k-step (HALF: of the k-tile's two). In the shadow of their first half the other register set is
+  // read (the next k-step, from S). This wave's loads of half HALF of a later k-tile go out to ``into`` beside
+  // them, as early as there is room between two products.
+  auto multiply = [&](auto HALF, const char* S, uint32_t into) {
+    constexpr int set = decltype(HALF)::value, H = P / 2;
     each<P>([&](auto I) {
       constexpr int i = decltype(I)::value, f = i / MB, b = i % MB;
       acc[f][b] = T::mfma16(wf[set][f], xf[set][b], acc[f][b]);
       if constexpr (i < H) {
         constexpr int r = (i * R + H - 1) / H;  // read r goes after product r H / R
-        if constexpr (r < R && r * H / R == i) read1(r, stage, 1 - set);
-      } else {
-        each<LPS>([&](auto L) {
-          constexpr int l = decltype(L)::value, at = H + l * H / LPS, gap = H / LPS / 2 > 0 ? H / LPS / 2 : 1;
-          if constexpr (at == i) put<decltype(target(L))::value>(place(l) + into);
-          if constexpr (at + gap == i) with(L, fetch);
-        });
+        if constexpr (r < R && r * H / R == i) read1(r, S, 1 - set);
       }
+      each<LPS>([&](auto L) {
+        constexpr int l = decltype(L)::value, at = ((2 * l + 1) * H / (2 * LPS)) | 1;
+        if constexpr (at == i) put<decltype(target(L))::value>(place(l) + into);
+        if constexpr (at + 1 == i) with(HALF, L, fetch);
+      });
       __builtin_amdgcn_sched_barrier(0);
     });
   };
-  // The k-tile past K first, then kt0, ..; k-tile q of that order is in stage q % ST. While q is multiplied, q and
-  // q + 1 are there and up to q + ST - 1 on the way: a wave waits for all but its newest ST - 3 k-tiles' loads.
-  auto landed = [&]() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LPS * (ST - 3)) : "memory"); };
+  // The k-tile past K first, then kt0, ..; k-tile q of that order is in slots 2 q and 2 q + 1 (mod ST). Its second
+  // k-step's fragments are read beside its first products; then its slots are free. Beside its first products
+  // half 0 of k-tile q + 2 goes out, to the fifth slot, beside its second ones half 1, to its own first slot. The next
+  // k-tile has to be there before the second products: all but the newest half.
+  const int KS = kt1 - kt0 + (tail ? 1 : 0);
   if (tail) stage_tail();
   if (left <= 0) none_left();
-  each<ST - 1>([&](auto Q) {
+  each<2>([&](auto Q) {
     constexpr int q = decltype(Q)::value;
     if (q > 0 || !tail) {
-      each<LPS>([&](auto i) {
-        with(i, [&](u32x4 r, uint32_t voff, uint32_t soff) {
-          put_fetch<decltype(target(i))::value>(place(decltype(i)::value) + q * STAGE, r, voff, soff);
+      each<2>([&](auto h) {
+        each<LPS>([&](auto i) {
+          with(h, i, [&](u32x4 r, uint32_t voff, uint32_t soff) {
+            put_fetch<decltype(target(i))::value>(place(decltype(i)::value) + (2 * q + decltype(h)::value) * SLOT, r,
+                                                  voff, soff);
+          });
         });
       });
       advance();
     }
   });
-  landed();
-  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(2 * LPS) : "memory");
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
+  auto up = [&](uint32_t x) { return x + SLOT == ST * SLOT ? 0u : x + SLOT; };
+  uint32_t cur = 0;  // the k-tile's first slot
+  auto at = [&](uint32_t first) { return lds + (second ? up(first) : first); };
 #pragma unroll
-  for (int i = 0; i < R; ++i) read1(i, 0, 0);
+  for (int i = 0; i < R; ++i) read1(i, at(0) + fa, 0);
   __builtin_amdgcn_sched_barrier(0);
-  uint32_t cur = 0, into = (ST - 1) * STAGE;
-  auto step = [&](auto SET) {
-    const uint32_t next = cur + STAGE == ST * STAGE ? 0 : cur + STAGE;
-    multiply(SET, next, into);  // everyone is done with k-tile q - 1, whose stage takes q + ST - 1
-    advance();
-    landed();
+  auto step = [&]() {
+    const uint32_t next = up(up(cur));
+    multiply(std::integral_constant<int, 0>{}, at(cur) + (fa ^ 64), up(up(next)));
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(LPS) : "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
-    into = cur;
+    multiply(std::integral_constant<int, 1>{}, at(next) + fa, cur);
+    advance();
     cur = next;
   };
   // the accumulators are in AGPRs: without this the compiler moves some out in the loop
@@ -179,10 +195,7 @@ __global__ void __launch_bounds__(TT, MB* NB == 16 ? 2 : 1) tile_kernel(Args a) 
       for (int b = 0; b < MB; ++b) asm volatile("" : "+a"(acc[f][b]));
   };
   pin();
-  for (int q = 0; q < KT; q += 2) {
-    step(std::integral_constant<int, 0>{});
-    if (q + 1 < KT) step(std::integral_constant<int, 1>{});
-  }
+  for (int q = 0; q < KS; ++q) step();
   pin();
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
@@ -193,8 +206,8 @@ __global__ void __launch_bounds__(TT, MB* NB == 16 ? 2 : 1) tile_kernel(Args a) 
   }
 
   // ---- epilogue, each wave for itself: ER rows at a time through its piece of LDS
-  constexpr int ER = 64, ELD = 16 * NB + 4;
-  static_assert(4 * ER * ELD * 4 <= tile_lds(MB, NB) && MB % 4 == 0, "the epilogue's LDS");
+  constexpr int ELD = 16 * NB + 4;
+  static_assert(MB % 4 == 0 && NB % 4 == 0, "");
   constexpr int LPR = GATED ? NB : 2 * NB, RPP = kWave / LPR, PB = 4;  // lanes of a row, rows of a pass, passes in flight
   float* tl = reinterpret_cast<float*>(lds) + wave * ER * ELD;
   const int fc = lane % LPR * 8, n = n0 + wn * (GATED ? NB * 8 : NB * 16) + fc;
