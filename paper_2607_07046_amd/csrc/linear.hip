@@ -1,8 +1,10 @@
 // Projections of a batch's rows: the host side of vt_linear and vt_linear_gated (the
-// kernels are in linear_thin.hip).
+// kernels are in linear_thin.hip, linear_mid.hip and linear_tile.hip).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <iterator>
+#include <limits>
 
 #include "linear.hpp"
 
@@ -34,33 +36,65 @@ vt_status check_shape(const vt_linear_io* io) {
   return VT_OK;
 }
 
+// Which kernel takes a product, and in how many slices of K: the one with the shortest modelled time (us)
+//   start + step * rounds * steps + tile * rounds + memory * MB + l2 * tile MB
+//   + (slices > 1) (join + part * slices' MB + slice * slices):
+// rounds of 256 workgroups (one per compute unit; those that fit beside each other overlap in ``step``), steps of 64 k of a
+// slice, MB read and written once, MB that the tiles load. The constants are fitted to 4000 products of random sizes (1 to 8192
+// rows, 64 to 16384 in, 16 to 32768 out, both kinds, every kernel and slice count): median error 4 to 8%, the
+// choice 1.8% slower than the best of all measured on average, 7% in one of ten, 23% in one of a hundred.
+// Without the kernel named the products are slower by (mean, worst): thin 1.3%, 1.2 times; 32 rows 0.8%, 1.3; 64 rows
+// 0.8%, 1.1; 64 x 128 0.5%, 1.25; 256 x 128 0.5%, 1.5; 256 x 256 0.7%, 1.5; 128 x 128 0.3%, 1.2; 16 x 64 0.2%, 1.1.
+struct Cost {
+  double start, step, tile, memory, l2, join, part, slice;
+};
+constexpr Cost kThinCost = {3.407, 0.0566, 0.156, 0.1243, 0.0, 1.275, 1.487, 0.097};
+constexpr Cost kMidCost[] = {{3.439, 0.1371, 0.151, 0.0975, 0.0, 1.111, 0.427, 0.066},
+                             {3.073, 0.1447, 0.360, 0.0973, 0.0, 1.220, 0.322, 0.097},
+                             {2.863, 0.1901, 0.825, 0.0530, 0.00912, 1.480, 0.266, 0.136},
+                             {1.706, 0.2589, 2.297, 0.0731, 0.01407, 2.096, 0.260, 0.240},
+                             {1.794, 0.4144, 3.204, 0.0268, 0.02384, 2.011, 0.182, 0.583}};
+constexpr Cost kTileCost[] = {{3.620, 0.5503, 5.360, 0.0649, 0.02155, 0, 0, 0},
+                              {5.131, 0.9108, 9.962, 0.0434, 0.02568, 0, 0, 0}};
+constexpr int kSlices[] = {1, 2, 3, 4, 6, 8, 12, 16};
+constexpr int kThinRows = 16;  // beyond, the thin tile reads the weights more than once
+
 struct Plan {
-  bool tile;   // 256 x 256 tiles
-  int mb, ob;  // else 16-row and 16-feature blocks of a tile
+  int kernel;  // -1: thin, then those of kMid, then of kTile
   int m_tiles, n_tiles, splits, steps;
+  double us;
 };
 
 Plan plan_of(int64_t M, int64_t N, int64_t K, bool gated) {
-  Plan p{};
-  if (M > 256) {
-    p.tile = true;
-    p.m_tiles = static_cast<int>((M + 255) / 256);
-    p.n_tiles = static_cast<int>(gated ? (N + 127) / 128 : (N + 255) / 256);
-    p.splits = 1;
-    return p;
-  }
-  p.mb = M <= 16 ? 1 : (M <= 32 ? 2 : 4);
-  p.ob = 1;
-  p.m_tiles = static_cast<int>((M + 16 * p.mb - 1) / (16 * p.mb));
-  p.n_tiles = static_cast<int>((N + 16 * p.ob - 1) / (16 * p.ob));
-  const int64_t steps = (K + 63) / 64, tiles = static_cast<int64_t>(p.m_tiles) * p.n_tiles;
-  int64_t splits = std::max<int64_t>(1, std::min<int64_t>(256 / tiles, steps / 16));
-  const int64_t tile_bytes = 4 * 256 * static_cast<int64_t>(p.mb) * p.ob * (gated ? 2 : 1);
-  splits = std::min<int64_t>(splits, std::max<int64_t>(1, static_cast<int64_t>(lin::kPartBytes) / (tile_bytes * tiles)));
-  if (tiles > lin::kMaxTiles) splits = 1;
-  p.steps = static_cast<int>((steps + splits - 1) / splits);
-  p.splits = static_cast<int>((steps + p.steps - 1) / p.steps);
-  return p;
+  Plan best{};
+  best.us = std::numeric_limits<double>::infinity();
+  const int64_t all = (K + 63) / 64;
+  const double mb = 2e-6 * (static_cast<double>(N) * K * (gated ? 2 : 1) + static_cast<double>(M) * (K + N));
+  auto consider = [&](int kernel, lin::Shape shape, const Cost& c, bool split) {
+    const bool thin = kernel < 0;
+    const int64_t out = gated && !thin ? shape.features / 2 : shape.features;
+    const int64_t wrows = gated && thin ? 2 * shape.features : shape.features;  // weight rows of a tile
+    const int64_t mt = (M + shape.rows - 1) / shape.rows, nt = (N + out - 1) / out, tiles = mt * nt;
+    int64_t last = 0;
+    for (int want : kSlices) {
+      if (want > 1 && (!split || tiles > lin::kMaxTiles)) break;
+      const int64_t steps = (all + want - 1) / want, splits = (all + steps - 1) / steps, work = tiles * splits;
+      const int64_t part = splits > 1 ? 4 * work * shape.rows * wrows : 0;
+      if (splits == last || part > static_cast<int64_t>(lin::kPartBytes)) continue;
+      last = splits;
+      const double rounds = static_cast<double>((work + 255) / 256);
+      const double loads = 128e-6 * static_cast<double>(work) * steps * (shape.rows + wrows);
+      const double us = c.start + rounds * (c.step * steps + c.tile) + c.memory * mb + c.l2 * loads +
+                        (splits > 1 ? c.join + c.part * 1e-6 * part + c.slice * splits : 0.0);
+      if (us < best.us)
+        best = {kernel, static_cast<int>(mt), static_cast<int>(nt), static_cast<int>(splits), static_cast<int>(steps), us};
+    }
+  };
+  if (M <= kThinRows) consider(-1, lin::kThin, kThinCost, true);
+  int kernel = 0;
+  for (size_t i = 0; i < std::size(lin::kMid); ++i) consider(kernel++, lin::kMid[i], kMidCost[i], true);
+  for (size_t i = 0; i < std::size(lin::kTile); ++i) consider(kernel++, lin::kTile[i], kTileCost[i], false);
+  return best;
 }
 
 vt_status project(const vt_linear_io* io, bool gated, void* ws, size_t ws_bytes, void* stream) {
@@ -109,11 +143,14 @@ vt_status project(const vt_linear_io* io, bool gated, void* ws, size_t ws_bytes,
   a.steps = p.steps;
   a.arrived = static_cast<uint32_t*>(ws);
   a.part = reinterpret_cast<float*>(static_cast<char*>(ws) + lin::kSyncBytes);
-  if ((static_cast<int64_t>(p.n_tiles) * p.splits + 7) / 8 * 8 * p.m_tiles >= (int64_t(1) << 23))  // 2^32 threads
+  if (lin::grid_of(p.m_tiles, static_cast<int64_t>(p.n_tiles) * p.splits) >= (int64_t(1) << 23))  // 2^32 threads
     return fail(VT_ERR_UNSUPPORTED, "%d x %d tiles: fewer rows or features per call", p.m_tiles, p.n_tiles);
   const bool bf16 = io->type == VT_T_BF16;
   const hipStream_t s = static_cast<hipStream_t>(stream);
-  const hipError_t e = p.tile ? lin::launch_tile(a, bf16, gated, s) : lin::launch_thin(a, bf16, gated, p.mb, p.ob, s);
+  constexpr int mids = static_cast<int>(std::size(lin::kMid));
+  const hipError_t e = p.kernel < 0      ? lin::launch_thin(a, bf16, gated, s)
+                       : p.kernel < mids ? lin::launch_mid(a, p.kernel, bf16, gated, s)
+                                         : lin::launch_tile(a, p.kernel > mids, bf16, gated, s);
   return e == hipSuccess ? VT_OK : fail(VT_ERR_HIP, "projection launch: %s", hipGetErrorString(e));
 }
 

@@ -1,6 +1,9 @@
 // Shared by the kernels of vt_linear and vt_linear_gated: arguments and epilogue.
 #pragma once
 
+#include <atomic>
+#include <type_traits>
+
 #include "device.hpp"
 #include "internal.hpp"
 #include "paged.hpp"
@@ -32,6 +35,22 @@ struct Args {
 constexpr int kMaxTiles = 4096;  // of a split product
 constexpr size_t kSyncBytes = kMaxTiles * sizeof(uint32_t);
 constexpr size_t kPartBytes = size_t(64) << 20;
+
+// This workgroup's tile: row of tiles and column (of the weights, and of its slices). Workgroups go round the XCDs one by
+// one; each XCD gets one run of the tiles in the order of blocks of 2048 rows, column by column in them, so
+// that the tiles running there at once share rows and weights in its L2. False: a workgroup too many.
+constexpr int kXcds = 8;
+inline int64_t grid_of(int64_t m_tiles, int64_t cols) { return (m_tiles * cols + kXcds - 1) / kXcds * kXcds; }
+__device__ __forceinline__ bool my_tile(int m_tiles, int cols, int tile_rows, int& m, int& col) {
+  const int all = m_tiles * cols, run = (all + kXcds - 1) / kXcds, id = blockIdx.x;
+  const int at = id % kXcds * run + id / kXcds;
+  if (at >= all) return false;
+  const int high = min(m_tiles, max(1, 2048 / tile_rows)), blk = at / (high * cols);
+  const int rows = min(high, m_tiles - blk * high), in = at - blk * high * cols;
+  col = in / rows;
+  m = blk * high + in % rows;
+  return true;
+}
 
 // The activation functions in fp32. Half a step of the results' type is 2^-12 at least; exp2 and
 // the reciprocal are the hardware's, a few 2^-24 off.
@@ -80,6 +99,15 @@ __device__ __forceinline__ void activate(float (&z)[W], int act) {
   }
 }
 
+// f(integral_constant 0), .., f(integral_constant N - 1)
+template <int N, int I = 0, class F>
+__device__ __forceinline__ void each(F&& f) {
+  if constexpr (I < N) {
+    f(std::integral_constant<int, I>{});
+    each<N, I + 1>(f);
+  }
+}
+
 template <class T>
 __device__ __forceinline__ float one(const uint16_t* p) {
   float a, b;
@@ -89,26 +117,29 @@ __device__ __forceinline__ float one(const uint16_t* p) {
 
 // W (4 or 8) consecutive features n.. of row m, from the product's sums to y. Whole groups by wide
 // accesses; the group that reaches past N by single numbers, so no byte outside is read or written
-// but a row's own.
+// but a row's own. (Both paths end in the same vector:
+// stores to z and u on either side of the branch were merged into one at a variable index, in scratch memory.)
 template <class T, bool GATED, int W>
 __device__ __forceinline__ void finish(const Args& a, int m, int n, float (&z)[W], float (&u)[W]) {
   typedef unsigned int vec __attribute__((ext_vector_type(W / 2)));
   const bool whole = n + W <= a.N;
   auto add = [&](const uint16_t* p, float (&to)[W]) {
+    vec v;
     if (whole) {
-      const vec v = *reinterpret_cast<const vec*>(p);
-#pragma unroll
-      for (int e = 0; e < W / 2; ++e) {
-        float lo, hi;
-        T::unpack2(v[e], lo, hi);
-        to[2 * e] += lo;
-        to[2 * e + 1] += hi;
-      }
+      v = *reinterpret_cast<const vec*>(p);
     } else {
-#pragma unroll
-      for (int e = 0; e < W; ++e)
-        if (n + e < a.N) to[e] += one<T>(p + e);
+      each<W / 2>([&](auto E) {
+        constexpr int e = decltype(E)::value;
+        v[e] = (n + 2 * e < a.N ? p[2 * e] : 0u) | (n + 2 * e + 1 < a.N ? static_cast<uint32_t>(p[2 * e + 1]) << 16 : 0u);
+      });
     }
+    each<W / 2>([&](auto E) {
+      constexpr int e = decltype(E)::value;
+      float lo, hi;
+      T::unpack2(v[e], lo, hi);
+      to[2 * e] += lo;
+      to[2 * e + 1] += hi;
+    });
   };
   if (a.bias[0]) add(a.bias[0] + n, z);
   activate(z, a.act);
@@ -120,14 +151,17 @@ __device__ __forceinline__ void finish(const Args& a, int m, int n, float (&z)[W
   if (a.res) add(a.res + m * a.ld_r + n, z);
   uint16_t* y = a.y + m * a.ld_y + n;
   vec v;
-#pragma unroll
-  for (int e = 0; e < W / 2; ++e) v[e] = T::pack2(z[2 * e], z[2 * e + 1]);
+  each<W / 2>([&](auto E) {
+    constexpr int e = decltype(E)::value;
+    v[e] = T::pack2(z[2 * e], z[2 * e + 1]);
+  });
   if (whole) {
     *reinterpret_cast<vec*>(y) = v;
   } else {
-#pragma unroll
-    for (int e = 0; e < W; ++e)
+    each<W>([&](auto E) {
+      constexpr int e = decltype(E)::value;
       if (n + e < a.N) y[e] = static_cast<uint16_t>(v[e / 2] >> (16 * (e % 2)));
+    });
   }
 }
 
@@ -144,8 +178,36 @@ __device__ __forceinline__ u32x4 load_at(rsrc_t r, uint32_t lane_off, uint32_t o
   return __builtin_amdgcn_raw_buffer_load_b128(r, lane_off, off, 0);
 }
 
-hipError_t launch_tile(const Args& a, bool bf16, bool gated, hipStream_t s);
-hipError_t launch_thin(const Args& a, bool bf16, bool gated, int mb, int ob, hipStream_t s);
+// The kernels' tiles: rows, and features (of a gated product half as many, but on the thin tile).
+struct Shape {
+  int rows, features;
+};
+constexpr Shape kThin = {16, 16};
+constexpr Shape kMid[] = {{16, 64}, {32, 64}, {64, 64}, {64, 128}, {128, 128}};
+constexpr Shape kTile[] = {{256, 128}, {256, 256}};
+
+// Dynamic LDS above 64 KiB has to be asked for, kernel by kernel, once per device.
+class LdsOnce {
+  std::atomic<bool> done_[64] = {};
+
+ public:
+  template <class F>
+  hipError_t operator()(F&& all) {
+    int dev = 0;
+    hipError_t e = hipGetDevice(&dev);
+    if (e != hipSuccess || (dev < 64 && done_[dev].load(std::memory_order_acquire))) return e;
+    all([&](const void* kernel, int bytes) {
+      const hipError_t r = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+      if (r != hipSuccess) e = r;
+    });
+    if (e == hipSuccess && dev < 64) done_[dev].store(true, std::memory_order_release);
+    return e;
+  }
+};
+
+hipError_t launch_thin(const Args& a, bool bf16, bool gated, hipStream_t s);
+hipError_t launch_mid(const Args& a, int which, bool bf16, bool gated, hipStream_t s);   // of kMid
+hipError_t launch_tile(const Args& a, bool wide, bool bf16, bool gated, hipStream_t s);  // of kTile
 
 }  // namespace lin
 }  // namespace vt

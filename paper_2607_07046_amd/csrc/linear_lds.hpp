@@ -7,8 +7,6 @@
 // find it in different banks.
 #pragma once
 
-#include <type_traits>
-
 #include "linear.hpp"
 
 namespace vt {
@@ -66,15 +64,6 @@ __device__ __forceinline__ rsrc_t rsrc_of(u32x4 w) {
 
 __device__ __forceinline__ uint32_t lds_address(const void* p) {
   return static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) const char*)p));
-}
-
-// f(integral_constant 0), .., f(integral_constant N - 1)
-template <int N, int I = 0, class F>
-__device__ __forceinline__ void each(F&& f) {
-  if constexpr (I < N) {
-    f(std::integral_constant<int, I>{});
-    each<N, I + 1>(f);
-  }
 }
 
 // A slice's sums to the workspace, in register order; whichever workgroup of the tile counts itself last adds all

@@ -2,7 +2,7 @@
 // linear_thin.hip and linear_tile.hip.
 //
 // WR x WC waves of 16 MBW rows x 16 NBW weight rows each. Both operands come straight into LDS through a
-// ring of ST stages of 64 HS k, up to ST - 1 of them on the way, each number once per tile; the
+// ring of ST stages of 64 k, up to ST - 1 of them on the way, each number once per tile; the
 // waves wait for a stage by the count of their own loads and meet once per stage. Two workgroups
 // share a compute unit, so one multiplies while the other waits.
 //
@@ -19,18 +19,16 @@
 namespace vt {
 namespace lin {
 
-template <class T, bool GATED, int WR, int WC, int MBW, int NBW, int HS, int ST>
+template <class T, bool GATED, int WR, int WC, int MBW, int NBW, int ST>
 __global__ void __launch_bounds__(WR* WC* kWave) mid_kernel(Args a) {
   constexpr int NW = WR * WC, XB = WR * MBW, WB = WC * NBW;  // waves; 16-row blocks of rows and of weights
-  constexpr int UK = 2 * (XB + WB), U = HS * UK, LPS = U / NW;  // units (8 rows x 64 k) of 64 k and of a stage
+  constexpr int U = 2 * (XB + WB), LPS = U / NW;              // units (8 rows x 64 k) of a stage, loads of a wave
   constexpr int NBO = GATED ? NBW / 2 : NBW;                 // 16-feature blocks of a wave
-  constexpr int TM = 16 * XB, TN = 16 * WC * NBO, TK = 64 * HS, STAGE = U * 1024, PW = NBO % 2 ? 4 : 8;
+  constexpr int TM = 16 * XB, TN = 16 * WC * NBO, TK = 64, STAGE = U * 1024, PW = NBO % 2 ? 4 : 8;
   static_assert(U % NW == 0 && (!GATED || NBW % 2 == 0), "");
   extern __shared__ __attribute__((aligned(16))) char lds[];
-  // tiles of the same weights stand on one XCD, one after the other
-  const int id = blockIdx.x, j = id / 8;
-  const int m_tile = j % a.m_tiles, unit = j / a.m_tiles * 8 + id % 8;
-  if (unit >= a.n_tiles * a.splits) return;
+  int m_tile, unit;
+  if (!my_tile(a.m_tiles, a.n_tiles * a.splits, TM, m_tile, unit)) return;
   const int n_tile = unit % a.n_tiles, split = unit / a.n_tiles;
   const int m0 = m_tile * TM, n0 = n_tile * TN;
   const int t = threadIdx.x, lane = t % kWave, wave = __builtin_amdgcn_readfirstlane(t / kWave);
@@ -38,8 +36,7 @@ __global__ void __launch_bounds__(WR* WC* kWave) mid_kernel(Args a) {
   const bool tail = full * TK < a.K && full >= kt0 && full < kt0 + a.steps;
   const int KT = max(kt1 - kt0, 0) + (tail ? 1 : 0);
 
-  // This wave loads units wave, wave + NW, .. of a stage: unit v is half v % 2 of block v % UK / 2 of its 64 k
-  // v / UK, the rows' blocks first.
+  // This wave loads units wave, wave + NW, .. of a stage: unit v is half v % 2 of block v / 2, the rows' first.
   const int rows_x = min(TM, a.M - m0), rows_w = min(TN, a.N - n0);
   const u32x4 rx = rsrc_words(a.x + m0 * a.ld_x, static_cast<uint32_t>(rows_x * a.ld_x * 2));
   const u32x4 rw0 = rsrc_words(a.w[0] + n0 * a.ld_w[0], static_cast<uint32_t>(rows_w * a.ld_w[0] * 2));
@@ -48,7 +45,7 @@ __global__ void __launch_bounds__(WR* WC* kWave) mid_kernel(Args a) {
   uint32_t off[LPS];
 #pragma unroll
   for (int i = 0; i < LPS; ++i) {
-    const int v = wave + NW * i, b = v % UK / 2, half = v % 2, brow = 8 * half + block_row(lane);
+    const int v = wave + NW * i, b = v / 2, half = v % 2, brow = 8 * half + block_row(lane);
     if (b < XB) {
       rs[i] = rx;
       off[i] = static_cast<uint32_t>(min(16 * b + brow, rows_x - 1) * a.ld_x * 2);
@@ -60,7 +57,7 @@ __global__ void __launch_bounds__(WR* WC* kWave) mid_kernel(Args a) {
       rs[i] = up ? rw1 : rw0;
       off[i] = static_cast<uint32_t>(row * (up ? a.ld_w[1] : a.ld_w[0]) * 2);
     }
-    off[i] += v / UK * 128 + block_chunk(lane, half) * 16;
+    off[i] += block_chunk(lane, half) * 16;
   }
   const uint32_t place0 = lds_address(lds) + wave * 1024;
   int next = kt0, left = kt1 - kt0;
@@ -88,7 +85,7 @@ __global__ void __launch_bounds__(WR* WC* kWave) mid_kernel(Args a) {
   if (tail) {  // to stage 0, with zeros past K
 #pragma unroll
     for (int i = 0; i < LPS; ++i) {
-      const int u = wave + NW * i, k = full * TK + u / UK * 64 + block_chunk(lane, u % 2) * 8;
+      const int u = wave + NW * i, k = full * TK + block_chunk(lane, u % 2) * 8;
       const u32x4 v = load_at(rsrc_of(rs[i]), off[i] | (k < a.K ? 0u : kOOB), full * (TK * 2));
       *reinterpret_cast<u32x4*>(lds + u * 1024 + lane * 16) = keep_first(v, a.K - k);
     }
@@ -105,8 +102,8 @@ __global__ void __launch_bounds__(WR* WC* kWave) mid_kernel(Args a) {
     asm volatile("" ::: "memory");
     load(into);
 #pragma unroll
-    for (int h = 0; h < 2 * HS; ++h) {
-      const char* S = lds + cur + h / 2 * UK * 1024 + (fa ^ (h % 2 * 64));
+    for (int h = 0; h < 2; ++h) {
+      const char* S = lds + cur + (fa ^ (h * 64));
       u32x4 xf[MBW], wf[NBW];
 #pragma unroll
       for (int b = 0; b < MBW; ++b) xf[b] = *reinterpret_cast<const u32x4*>(S + (wr * MBW + b) * 2048);
@@ -141,6 +138,40 @@ __global__ void __launch_bounds__(WR* WC* kWave) mid_kernel(Args a) {
       finish<T, GATED, PW>(a, m, n, z, u);
     }
   }
+}
+
+namespace {
+
+struct Kernel {
+  void (*run[4])(Args);  // fp16, fp16 gated, bf16, bf16 gated
+  int threads, lds;
+};
+
+template <int WR, int WC, int MBW, int NBW, int ST>
+constexpr Kernel kernel() {
+  return {{mid_kernel<Half, false, WR, WC, MBW, NBW, ST>, mid_kernel<Half, true, WR, WC, MBW, NBW, ST>,
+           mid_kernel<BFloat, false, WR, WC, MBW, NBW, ST>, mid_kernel<BFloat, true, WR, WC, MBW, NBW, ST>},
+          WR * WC * kWave,
+          ST * 2 * (WR * MBW + WC * NBW) * 1024};
+}
+
+// in the order of kMid
+const Kernel kKernels[] = {kernel<1, 2, 1, 2, 5>(), kernel<2, 2, 1, 2, 4>(), kernel<4, 2, 1, 2, 4>(),
+                           kernel<4, 2, 1, 4, 4>(), kernel<4, 2, 2, 4, 4>()};
+
+}  // namespace
+
+hipError_t launch_mid(const Args& a, int which, bool bf16, bool gated, hipStream_t s) {
+  static LdsOnce once;
+  const hipError_t e = once([](auto&& raise) {
+    for (const Kernel& k : kKernels)
+      for (auto* f : k.run) raise(reinterpret_cast<const void*>(f), k.lds);
+  });
+  if (e != hipSuccess) return e;
+  const Kernel& k = kKernels[which];
+  hipLaunchKernelGGL(k.run[2 * bf16 + gated], dim3(static_cast<uint32_t>(grid_of(a.m_tiles, a.n_tiles * a.splits))),
+                     dim3(k.threads), k.lds, s, a);
+  return hipGetLastError();
 }
 
 }  // namespace lin

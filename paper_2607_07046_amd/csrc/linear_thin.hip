@@ -1,7 +1,7 @@
 // Products of few rows with a large weight matrix: vt_linear and vt_linear_gated while their time is that
 // of reading the weights.
 //
-// A workgroup takes a tile of 16 MB rows and 16 OB features; its waves share out the k-steps of
+// A workgroup takes a tile of 16 rows and 16 features; its waves share out the k-steps of
 // its slice of K (64 k each, in turn, so that together they read whole pieces of a weight row), and each
 // multiplies weights and activations straight from memory: both operands of a 16 x 16 x 32 matrix
 // instruction are 16 bytes per lane of consecutive k, and nothing is used by two waves, so LDS would
@@ -12,16 +12,18 @@
 namespace vt {
 namespace lin {
 
-template <class T, bool GATED, int MB, int OB, int NW, int HS, int DEPTH>
+constexpr int NW = 8, HW = NW / 2;  // waves
+constexpr int HS = 2, KS = 32 * HS;  // matrix instructions' k-steps, and k, of a step
+constexpr int DEPTH = 2;             // steps in flight
+
+template <class T, bool GATED>
 __global__ void __launch_bounds__(NW* kWave) thin_kernel(Args a) {
-  constexpr int KS = 32 * HS;  // k of a step
-  constexpr int FB = GATED ? 2 * OB : OB, TN = 16 * OB, TM = 16 * MB, LD = 16 * FB + 4, HW = NW / 2;
+  constexpr int FB = GATED ? 2 : 1, TN = kThin.features, TM = kThin.rows, LD = 16 * FB + 4;  // FB: weight matrices
+  static_assert(TN == 16 && TM == 16, "one fragment of each");
   __shared__ __attribute__((aligned(16))) float red[HW * TM * LD];
   __shared__ uint32_t ticket;
-  // tiles of the same weights stand on one XCD, one after the other
-  const int id = blockIdx.x, j = id / 8;
-  const int m_tile = j % a.m_tiles, unit = j / a.m_tiles * 8 + id % 8;
-  if (unit >= a.n_tiles * a.splits) return;
+  int m_tile, unit;
+  if (!my_tile(a.m_tiles, a.n_tiles * a.splits, TM, m_tile, unit)) return;
   const int n_tile = unit % a.n_tiles, split = unit / a.n_tiles;
   const int m0 = m_tile * TM, n0 = n_tile * TN;
   const int t = threadIdx.x, lane = t % kWave, wave = __builtin_amdgcn_readfirstlane(t / kWave);
@@ -31,45 +33,33 @@ __global__ void __launch_bounds__(NW* kWave) thin_kernel(Args a) {
   const rsrc_t rx = make_rsrc(a.x + m0 * a.ld_x, static_cast<uint32_t>(rows_x * a.ld_x * 2));
   auto weights = [&](int i) { return make_rsrc(a.w[i] + n0 * a.ld_w[i], static_cast<uint32_t>(rows_w * a.ld_w[i] * 2)); };
   const rsrc_t rw0 = weights(0), rw1 = GATED ? weights(1) : rw0;
-  uint32_t ow[FB], ox[MB];
+  uint32_t ow[FB];
 #pragma unroll
-  for (int b = 0; b < FB; ++b) {
-    const int row = 16 * (b % OB) + r;
-    ow[b] = row < rows_w ? static_cast<uint32_t>(row * a.ld_w[b / OB] * 2) + q * 16 : kOOB;
-  }
-#pragma unroll
-  for (int b = 0; b < MB; ++b) {
-    const int row = 16 * b + r;
-    ox[b] = row < rows_x ? static_cast<uint32_t>(row * a.ld_x * 2) + q * 16 : kOOB;
-  }
+  for (int f = 0; f < FB; ++f) ow[f] = r < rows_w ? static_cast<uint32_t>(r * a.ld_w[f] * 2) + q * 16 : kOOB;
+  const uint32_t ox = r < rows_x ? static_cast<uint32_t>(r * a.ld_x * 2) + q * 16 : kOOB;
 
-  f32x4 acc[FB][MB];
+  f32x4 acc[FB];
 #pragma unroll
-  for (int f = 0; f < FB; ++f)
-#pragma unroll
-    for (int b = 0; b < MB; ++b) acc[f][b] = f32x4{0.f, 0.f, 0.f, 0.f};
-  u32x4 wf[DEPTH][FB][HS], xf[DEPTH][MB][HS];
+  for (int f = 0; f < FB; ++f) acc[f] = f32x4{0.f, 0.f, 0.f, 0.f};
+  u32x4 wf[DEPTH][FB][HS], xf[DEPTH][HS];
   const int full = a.K / KS, s0 = split * a.steps;
   const int s1 = min(s0 + a.steps, full);
   // step i of this wave; past the slice's end nothing is read and zeros are multiplied
-  auto load = [&](int i, u32x4 (&w)[FB][HS], u32x4 (&x)[MB][HS]) {
+  auto load = [&](int i, u32x4 (&w)[FB][HS], u32x4 (&x)[HS]) {
     const int s = s0 + wave + i * NW;
     const uint32_t gone = s < s1 ? 0u : kOOB, at = s < s1 ? static_cast<uint32_t>(s * KS * 2) : 0u;
 #pragma unroll
     for (int h = 0; h < HS; ++h) {
 #pragma unroll
-      for (int f = 0; f < FB; ++f) w[f][h] = load_at(f < OB ? rw0 : rw1, ow[f] | gone, at + h * 64);
-#pragma unroll
-      for (int b = 0; b < MB; ++b) x[b][h] = load_at(rx, ox[b] | gone, at + h * 64);
+      for (int f = 0; f < FB; ++f) w[f][h] = load_at(f ? rw1 : rw0, ow[f] | gone, at + h * 64);
+      x[h] = load_at(rx, ox | gone, at + h * 64);
     }
   };
-  auto multiply = [&](const u32x4 (&w)[FB][HS], const u32x4 (&x)[MB][HS]) {
+  auto multiply = [&](const u32x4 (&w)[FB][HS], const u32x4 (&x)[HS]) {
 #pragma unroll
     for (int h = 0; h < HS; ++h)
 #pragma unroll
-      for (int f = 0; f < FB; ++f)
-#pragma unroll
-        for (int b = 0; b < MB; ++b) acc[f][b] = T::mfma16(w[f][h], x[b][h], acc[f][b]);
+      for (int f = 0; f < FB; ++f) acc[f] = T::mfma16(w[f][h], x[h], acc[f]);
   };
   const int mine = s0 + wave < s1 ? (s1 - s0 - wave + NW - 1) / NW : 0;
 #pragma unroll
@@ -89,30 +79,25 @@ __global__ void __launch_bounds__(NW* kWave) thin_kernel(Args a) {
       const uint32_t gone = k < a.K ? 0u : kOOB;
 #pragma unroll
       for (int f = 0; f < FB; ++f)
-        wf[0][f][h] = keep_first(load_at(f < OB ? rw0 : rw1, ow[f] | gone, full * KS * 2 + h * 64), a.K - k);
-#pragma unroll
-      for (int b = 0; b < MB; ++b) xf[0][b][h] = keep_first(load_at(rx, ox[b] | gone, full * KS * 2 + h * 64), a.K - k);
+        wf[0][f][h] = keep_first(load_at(f ? rw1 : rw0, ow[f] | gone, full * KS * 2 + h * 64), a.K - k);
+      xf[0][h] = keep_first(load_at(rx, ox | gone, full * KS * 2 + h * 64), a.K - k);
     }
     multiply(wf[0], xf[0]);
   }
 
-  // accumulator i of (f, b): feature 16 f + 4 q + i, row 16 b + r
-  auto place = [&](int w, int f, int b) { return reinterpret_cast<f32x4*>(red + (w * TM + 16 * b + r) * LD + 16 * f + 4 * q); };
+  // accumulator i of f: feature 4 q + i, row r
+  auto place = [&](int w, int f) { return reinterpret_cast<f32x4*>(red + (w * TM + r) * LD + 16 * f + 4 * q); };
   if (wave >= HW) {
 #pragma unroll
-    for (int f = 0; f < FB; ++f)
-#pragma unroll
-      for (int b = 0; b < MB; ++b) *place(wave - HW, f, b) = acc[f][b];
+    for (int f = 0; f < FB; ++f) *place(wave - HW, f) = acc[f];
   }
   __syncthreads();
   if (wave < HW) {
 #pragma unroll
-    for (int f = 0; f < FB; ++f)
-#pragma unroll
-      for (int b = 0; b < MB; ++b) {
-        f32x4* p = place(wave, f, b);
-        *p = acc[f][b] + *p;
-      }
+    for (int f = 0; f < FB; ++f) {
+      f32x4* p = place(wave, f);
+      *p = acc[f] + *p;
+    }
   }
   __syncthreads();
   auto sum4 = [&](int m, int n) __attribute__((always_inline)) {
@@ -126,10 +111,10 @@ __global__ void __launch_bounds__(NW* kWave) thin_kernel(Args a) {
     finish<T, GATED, 4>(a, m0 + m, n0 + n, z, u);
   };
   const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
-  constexpr int UNITS = TM * OB * 4;
+  constexpr int UNITS = TM * TN / 4;
   if (a.splits == 1) {
     for (int i = t; i < UNITS; i += NW * kWave) {
-      const int m = i / (OB * 4), n = i % (OB * 4) * 4;
+      const int m = i / (TN / 4), n = i % (TN / 4) * 4;
       if (m >= rows_x || n >= rows_w) continue;
       out4(m, n, sum4(m, n), GATED ? sum4(m, TN + n) : zero);
     }
@@ -156,7 +141,7 @@ __global__ void __launch_bounds__(NW* kWave) thin_kernel(Args a) {
   if (ticket != static_cast<uint32_t>(a.splits - 1)) return;
   if (t == 0) sync_store(a.arrived + tile, 0u);
   for (int i = t; i < UNITS; i += NW * kWave) {
-    const int m = i / (OB * 4), n = i % (OB * 4) * 4;
+    const int m = i / (TN / 4), n = i % (TN / 4) * 4;
     if (m >= rows_x || n >= rows_w) continue;
     f32x4 z4 = zero, u4 = zero;
     const uint32_t at = static_cast<uint32_t>(m * FB * 16 + n) * 4;
@@ -170,22 +155,11 @@ __global__ void __launch_bounds__(NW* kWave) thin_kernel(Args a) {
   }
 }
 
-namespace {
-
-template <class T, bool GATED>
-void (*pick(int mb, int ob))(Args) {
-  if (mb == 1) return thin_kernel<T, GATED, 1, 1, 8, 2, 4>;
-  if (mb == 2) return ob == 1 ? thin_kernel<T, GATED, 2, 1, 8, 2, 4> : thin_kernel<T, GATED, 2, 2, 8, 2, 2>;
-  return ob == 1 ? thin_kernel<T, GATED, 4, 1, 8, 2, 2> : thin_kernel<T, GATED, 4, 2, 8, 2, 2>;
-}
-
-}  // namespace
-
-hipError_t launch_thin(const Args& a, bool bf16, bool gated, int mb, int ob, hipStream_t s) {
-  auto* k = bf16 ? (gated ? pick<BFloat, true>(mb, ob) : pick<BFloat, false>(mb, ob))
-                 : (gated ? pick<Half, true>(mb, ob) : pick<Half, false>(mb, ob));
-  const int64_t units = static_cast<int64_t>(a.n_tiles) * a.splits;
-  hipLaunchKernelGGL(k, dim3(static_cast<uint32_t>((units + 7) / 8 * 8 * a.m_tiles)), dim3(8 * kWave), 0, s, a);
+hipError_t launch_thin(const Args& a, bool bf16, bool gated, hipStream_t s) {
+  void (*const kernels[])(Args) = {thin_kernel<Half, false>, thin_kernel<Half, true>, thin_kernel<BFloat, false>,
+                                   thin_kernel<BFloat, true>};
+  hipLaunchKernelGGL(kernels[2 * bf16 + gated], dim3(static_cast<uint32_t>(grid_of(a.m_tiles, a.n_tiles * a.splits))),
+                     dim3(NW * kWave), 0, s, a);
   return hipGetLastError();
 }
 

@@ -1,10 +1,10 @@
-// Products of many rows: vt_linear and vt_linear_gated on tiles of 256 rows x 256 features.
+// Products of many rows: vt_linear and vt_linear_gated on tiles of 256 rows x 256 or 128 weight rows.
 //
-// Four waves, one per SIMD, of 128 x 128 each (accumulators in all 256 AGPRs). Both operands go from memory
+// Four waves, one per SIMD, of 128 x 128 each (accumulators in all 256 AGPRs) or 128 x 64. Both operands go from memory
 // straight into LDS, 16 bytes a lane and 1 KiB an instruction, in k-tiles of 64 through a ring of five half-tiles;
 // a wave multiplies one k-step of 32 while it reads the next one's fragments and sends its share of the loads of a
 // k-tile further on, so that nothing stands between two products for longer than the first of them takes. A gated
-// product's weight blocks are four of the gate and four of the up projection in turn, 64 features of both for each wave, so a
+// product's weight blocks are half a wave's of the gate and half of the up projection in turn, for the same features, so a
 // feature's two sums are in the same lane.
 //
 // The product's first operand is the weights: a lane's four accumulators are then four consecutive features of a
@@ -13,16 +13,12 @@
 //
 // Rows past the matrices' ends are read from their last row (the sums are never stored). A last k-tile that
 // reaches past K goes through registers, masked, and is multiplied first.
-#include <mutex>
-#include <vector>
-
 #include "linear_lds.hpp"
 
 namespace vt {
 namespace lin {
 
 constexpr int TK = 64, TT = 256;
-constexpr int WALK_M = 8;  // row tiles of a block of an XCD's walk
 constexpr int ST = 5;      // slots of half a k-tile
 constexpr int ER = 64;     // rows of a wave in the epilogue's LDS
 
@@ -33,25 +29,18 @@ constexpr int tile_lds(int mb, int nb) {
 }
 
 // MB, NB: 16-row blocks of rows and of weights of a wave.
-template <class T, bool GATED, int MB, int NB, bool SPLIT>
-__global__ void __launch_bounds__(TT, MB* NB == 16 ? 2 : 1) tile_kernel(Args a) {
+template <class T, bool GATED, int MB, int NB>
+__global__ void __launch_bounds__(TT, 1) tile_kernel(Args a) {
   extern __shared__ __attribute__((aligned(16))) char lds[];
   constexpr int SLOT = slot_bytes(MB, NB), XB = 2 * MB * 1024;
   constexpr int TM = 32 * MB, TN = 32 * NB, NO = GATED ? TN / 2 : TN;  // rows, weight rows, features of a tile
   constexpr int P = MB * NB, R = MB + NB, LX = MB / 2, LPS = R / 2;    // products, reads, loads of a wave per half
-  // An XCD takes every eighth column of tiles, in blocks of WALK_M rows of them: the tiles that run there
-  // at once share rows and weights in its L2.
-  const int cols = SPLIT ? a.n_tiles * a.splits : a.n_tiles;
-  const int id = blockIdx.x, groups = (cols + 7) / 8, j = id / 8;
-  const int bm = min(a.m_tiles, WALK_M), blk = j / (bm * groups);
-  const int rows = min(bm, a.m_tiles - blk * bm), rr = j - blk * bm * groups;
-  const int col = rr / rows * 8 + id % 8, m_tile = blk * bm + rr % rows;
-  if (col >= cols) return;
-  const int n_tile = SPLIT ? col % a.n_tiles : col, split = SPLIT ? col / a.n_tiles : 0;
+  int m_tile, n_tile;
+  if (!my_tile(a.m_tiles, a.n_tiles, TM, m_tile, n_tile)) return;
   const int m0 = m_tile * TM, n0 = n_tile * NO;
   const int t = threadIdx.x, lane = t % kWave, wave = __builtin_amdgcn_readfirstlane(t / kWave);
-  const int full = a.K / TK, kt0 = SPLIT ? split * a.steps : 0, kt1 = SPLIT ? max(kt0, min(kt0 + a.steps, full)) : full;
-  const bool tail = full * TK < a.K && (!SPLIT || (full >= kt0 && full < kt0 + a.steps));
+  const int full = a.K / TK;
+  const bool tail = full * TK < a.K;
 
   const uint32_t lbase = lds_address(lds);
   // A slot holds the first or the last 8 rows of every 16-row block, 64 k wide; this wave loads a quarter of its
@@ -75,8 +64,8 @@ __global__ void __launch_bounds__(TT, MB* NB == 16 ? 2 : 1) tile_kernel(Args a) 
   }
   // A half's loads of this wave, the rows' first. Past the last k-tile they go on with empty
   // ranges from offset 0 (no memory traffic, slots that nobody reads), so the counts stay.
-  uint32_t koff = kt0 * (TK * 2);
-  int left = kt1 - kt0;
+  uint32_t koff = 0;
+  int left = full;
   const uint32_t placex = lbase + wave * LX * 1024, placew = lbase + XB + wave * (NB / 2) * 1024;
   auto place = [&](int i) { return i < LX ? placex : placew; };
   auto target = [](auto i) {
@@ -147,11 +136,11 @@ __global__ void __launch_bounds__(TT, MB* NB == 16 ? 2 : 1) tile_kernel(Args a) 
       __builtin_amdgcn_sched_barrier(0);
     });
   };
-  // The k-tile past K first, then kt0, ..; k-tile q of that order is in slots 2 q and 2 q + 1 (mod ST). Its second
+  // The k-tile past K first, then 0, 1, ..; k-tile q of that order is in slots 2 q and 2 q + 1 (mod ST). Its second
   // k-step's fragments are read beside its first products; then its slots are free. Beside its first products
   // half 0 of k-tile q + 2 goes out, to the fifth slot, beside its second ones half 1, to its own first slot. The next
   // k-tile has to be there before the second products: all but the newest half.
-  const int KS = kt1 - kt0 + (tail ? 1 : 0);
+  const int KT = full + (tail ? 1 : 0);
   if (tail) stage_tail();
   if (left <= 0) none_left();
   each<2>([&](auto Q) {
@@ -195,15 +184,10 @@ __global__ void __launch_bounds__(TT, MB* NB == 16 ? 2 : 1) tile_kernel(Args a) 
       for (int b = 0; b < MB; ++b) asm volatile("" : "+a"(acc[f][b]));
   };
   pin();
-  for (int q = 0; q < KS; ++q) step();
+  for (int q = 0; q < KT; ++q) step();
   pin();
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
-
-  if constexpr (SPLIT) {
-    if (!join<NB, MB, 4>(a, acc, lds, m_tile * a.n_tiles + n_tile, split, wave, lane)) return;
-    __syncthreads();
-  }
 
   // ---- epilogue, each wave for itself: ER rows at a time through its piece of LDS
   constexpr int ELD = 16 * NB + 4;
@@ -298,27 +282,21 @@ __global__ void __launch_bounds__(TT, MB* NB == 16 ? 2 : 1) tile_kernel(Args a) 
   });
 }
 
-// The kernels' dynamic LDS raised to what they use, once per device.
-hipError_t launch_tile(const Args& a, bool bf16, bool gated, hipStream_t s) {
-  static std::mutex mu;
-  static std::vector<char> ready;
-  void (*const kernels[])(Args) = {tile_kernel<Half, false, 8, 8, false>, tile_kernel<Half, true, 8, 8, false>,
-                                   tile_kernel<BFloat, false, 8, 8, false>, tile_kernel<BFloat, true, 8, 8, false>};
-  int dev = 0;
-  hipError_t e = hipGetDevice(&dev);
+hipError_t launch_tile(const Args& a, bool wide, bool bf16, bool gated, hipStream_t s) {
+  static LdsOnce once;
+  void (*const kernels[2][4])(Args) = {
+      {tile_kernel<Half, false, 8, 4>, tile_kernel<Half, true, 8, 4>, tile_kernel<BFloat, false, 8, 4>,
+       tile_kernel<BFloat, true, 8, 4>},
+      {tile_kernel<Half, false, 8, 8>, tile_kernel<Half, true, 8, 8>, tile_kernel<BFloat, false, 8, 8>,
+       tile_kernel<BFloat, true, 8, 8>}};
+  const int lds[] = {tile_lds(8, 4), tile_lds(8, 8)};
+  const hipError_t e = once([&](auto&& raise) {
+    for (int w = 0; w < 2; ++w)
+      for (auto* f : kernels[w]) raise(reinterpret_cast<const void*>(f), lds[w]);
+  });
   if (e != hipSuccess) return e;
-  {
-    std::lock_guard<std::mutex> lk(mu);
-    if (static_cast<int>(ready.size()) <= dev) ready.resize(dev + 1);
-    if (!ready[dev]) {
-      for (auto* k : kernels) {
-        e = hipFuncSetAttribute(reinterpret_cast<const void*>(k), hipFuncAttributeMaxDynamicSharedMemorySize, tile_lds(8, 8));
-        if (e != hipSuccess) return e;
-      }
-      ready[dev] = 1;
-    }
-  }
-  hipLaunchKernelGGL(kernels[2 * bf16 + gated], dim3((a.n_tiles + 7) / 8 * 8 * a.m_tiles), dim3(TT), tile_lds(8, 8), s, a);
+  hipLaunchKernelGGL(kernels[wide][2 * bf16 + gated], dim3(static_cast<uint32_t>(grid_of(a.m_tiles, a.n_tiles))),
+                     dim3(TT), lds[wide], s, a);
   return hipGetLastError();
 }
 

@@ -25,6 +25,14 @@ SHAPES = [(1, 1, 1), (1, 7, 5), (1, 8, 16), (1, 64, 17), (1, 65, 16), (1, 512, 1
           (300, 64, 300), (300, 90, 300), (300, 128, 130), (300, 161, 270), (300, 192, 600), (300, 224, 300), (2400, 200, 2500)]
 
 
+# for each tile of the kernels, whole and in slices of K, with ends of rows, features and K inside it
+LARGE = [(20, 898, 75), (2279, 1322, 9), (754, 1846, 30), (1089, 2307, 21), (2885, 130, 140), (2794, 2496, 30),
+         (3119, 2210, 17), (262, 37, 1836), (1577, 33, 673), (614, 3771, 769), (2575, 3719, 196), (663, 33, 3138),
+         (781, 100, 2565), (337, 4092, 2839), (90, 8193, 4141), (80, 5742, 3326), (1378, 256, 3918), (2171, 230, 2423),
+         (2337, 65, 2682), (3785, 33, 4161), (4115, 200, 3319), (3380, 1, 3699), (3869, 359, 3362), (2500, 448, 4008)]
+SHAPES += LARGE
+
+
 @BOTH
 @pytest.mark.parametrize("M,K,N", SHAPES)
 def test_shapes(ws, type, M, K, N):
@@ -52,10 +60,20 @@ def test_epilogue(ws, type, act, gated, M):
 
 
 @BOTH
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+@pytest.mark.parametrize("gated", [False, True])
+@pytest.mark.parametrize("M,K,N", LARGE)
+def test_epilogue_of_all_tiles(ws, type, act, gated, M, K, N):
+    x = Linear(type, M, min(K, 4200), N, act=act, bias=True, residual=True, gated=gated, seed=M)
+    x.call(ws)
+    x.check()
+
+
+@BOTH
 @pytest.mark.parametrize("bias,residual", [(True, False), (False, True)])
-@pytest.mark.parametrize("M", [1, 70, 260])
-def test_bias_or_residual(ws, type, bias, residual, M):
-    x = Linear(type, M, 72, 133, bias=bias, residual=residual, seed=3)
+@pytest.mark.parametrize("M,K,N", [(1, 72, 133), (70, 72, 133), (260, 72, 133), (1200, 70, 2565), (2400, 136, 4003)])
+def test_bias_or_residual(ws, type, bias, residual, M, K, N):
+    x = Linear(type, M, K, N, bias=bias, residual=residual, seed=3)
     x.call(ws)
     x.check()
 
@@ -84,7 +102,8 @@ def test_growing_sums(ws, type):
 
 
 @BOTH
-@pytest.mark.parametrize("M,K,N", [(1, 512, 96), (1, 9000, 40), (50, 512, 96), (260, 512, 300)])
+@pytest.mark.parametrize("M,K,N", [(1, 512, 96), (1, 9000, 40), (50, 512, 96), (260, 512, 300), (90, 8193, 4141),
+                                   (1200, 70, 2565), (2400, 136, 4003)])
 def test_residual_in_place(ws, type, M, K, N):
     x = Linear(type, M, K, N, act="gelu", residual=True, seed=9)
     before = x.residual.clone()
@@ -95,21 +114,21 @@ def test_residual_in_place(ws, type, M, K, N):
 
 
 @BOTH
-@pytest.mark.parametrize("M", [3, 60, 257, 600])
+@pytest.mark.parametrize("M,N", [(3, 301), (60, 301), (257, 301), (600, 301), (1200, 2565), (2000, 4005)])
 @pytest.mark.parametrize("gated", [False, True])
-def test_rows_and_features_apart(ws, type, M, gated):
+def test_rows_and_features_apart(ws, type, M, N, gated):
     """NaN and infinity in a row or a weight reach its own results and no others."""
-    x = Linear(type, M, 330, 301, gated=gated, act="silu" if gated else "none", seed=5)
+    x = Linear(type, M, 330, N, gated=gated, act="silu" if gated else "none", seed=5)
     x.call(ws)
     clean = x.y.clone()
     x.x[1, 329] = math.nan
-    x.w[300, 7] = math.inf
+    x.w[N - 1, 7] = math.inf
     x.call(ws)
     rows = torch.arange(M, device="cuda") != 1
-    assert torch.equal(x.y[rows][:, :300], clean[rows][:, :300])
+    assert torch.equal(x.y[rows][:, :N - 1], clean[rows][:, :N - 1])
     assert bool(x.y[1].isnan().all())
-    assert bool((~x.y[:, 300].isfinite()).sum() >= M // 4)  # silu(-inf) * u is NaN, inf stays, and some x are 0
-    assert bool((around(x.y)[:, 301:] == MARK).all())
+    assert bool((~x.y[:, N - 1].isfinite()).sum() >= M // 4)  # silu(-inf) * u is NaN, inf stays, and some x are 0
+    assert bool((around(x.y)[:, N:] == MARK).all())
 
 
 def test_overflow_of_f16(ws):
@@ -218,7 +237,8 @@ def test_two_streams():
 def test_graph_replays(ws):
     """One captured step of several projections, replayed on new inputs."""
     xs = [Linear("f16", 1, 4096, 64, seed=1), Linear("f16", 70, 4096, 48, residual=True, seed=2),
-          Linear("f16", 300, 512, 600, gated=True, act="silu", seed=3)]
+          Linear("f16", 300, 512, 600, gated=True, act="silu", seed=3), Linear("f16", 90, 8193, 4141, seed=4),
+          Linear("f16", 2171, 230, 2423, seed=5), Linear("f16", 2500, 448, 4008, bias=True, seed=6)]
     for x in xs:
         x.call(ws)
     graph = torch.cuda.CUDAGraph()
