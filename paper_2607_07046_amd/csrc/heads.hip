@@ -4,13 +4,15 @@
 
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "paged.hpp"
 
 namespace vt {
 namespace pg {
 
-constexpr int HT = 256;  // threads per workgroup
+
+constexpr int HT = 256, HW = HT / kWave;  // threads and waves per workgroup
 
 struct HeadsArgs {
   Pool p;                // paged only; n_kv key heads either way
@@ -25,19 +27,64 @@ struct HeadsArgs {
   int32_t n_q, half;     // query heads (0: none); pairs that turn
 };
 
-// A workgroup takes one row: 8 (head size 64) or 16 lanes a head, 8 numbers each, so a lane's part of the rotation is the
-// same for all heads that it gets and its angles are computed once. The head's sum of squares is
-// a sum over its lanes; with HALVES the number that a number turns with is in another lane and comes
-// through the wave's own piece of LDS (9 floats a lane, so that neither side has bank conflicts), wherever
-// the turned part of a head ends. Every number is read and written once; a lane's next heads are in flight
+// Eight numbers as e4m3: number / scale, rounded to nearest even, saturating; NaN stays. The quotient is the product
+// with the reciprocal and one correction, which leaves a division's result (an exact quotient that lies between
+// two e4m3 numbers must not move).
+__device__ __forceinline__ u32x2 scaled_to_f8(const float (&x)[8], float scale, float rcp) {
+  float y[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const float q = x[e] * rcp, d = fmaf(fmaf(-q, scale, x[e]), rcp, q);
+    y[e] = fabsf(q) > kF8Max ? copysignf(kF8Max, q) : d;
+  }
+  u32x2 r;
+#pragma unroll
+  for (int w = 0; w < 2; ++w) {
+    int t = __builtin_amdgcn_cvt_pk_fp8_f32(y[4 * w], y[4 * w + 1], 0, false);
+    r[w] = __builtin_amdgcn_cvt_pk_fp8_f32(y[4 * w + 2], y[4 * w + 3], t, true);
+  }
+  return r;
+}
+
+// A workgroup takes one row, or for few rows a part of its heads; a wave's turn is 512 numbers of them, 8 per lane.
+//   y_i = (x_i g_i) cos_i +- (x_j g_j) sin_i = inv (x_i A_i + x_j B_i),  j the number that i turns with:
+// A and B are the same for all of a row's query heads and for all of its key heads and are made once, in LDS.
+// With HALVES x_j is in another lane: the head's 16-bit numbers go through LDS, in one 16-byte read where the
+// halves are multiples of 8. Keys, values and queries start at whole turns of a wave, so what is done is the
+// same for all of its lanes. Every number is read and written once; the next turns' loads are in flight
 // while one is computed.
+// What bounds it: memory for many rows, the chain row -> sequence -> length -> page -> store for few. Measured: ragged
+// prompts, 10310 rows of 96 heads of 128, bf16 into 8-bit, half of each head turning: 94 us for 422 MB, 4.5 TB/s
+// (a wave per row 96 to 164, the slower the more of them were at work; with A, B and the angles in each
+// lane's registers 139); 4096 rows of 64 heads without a cache 29 us, 4.6 TB/s; 64 rows of 80 heads 4.0 us in a
+// captured graph, one row 2.9.
 template <class T, bool PAGED, bool F8, bool HALVES, int D>
-__global__ void __launch_bounds__(HT) heads_kernel(HeadsArgs a, Freq f) {
-  constexpr int CPR = D / 8, HL = HT / CPR, B = 4;
-  __shared__ float swap[HALVES ? HT * 9 : 1];
-  const int c = threadIdx.x % CPR, hl = threadIdx.x / CPR;
-  const int r = blockIdx.x, nkv = a.p.n_kv, nk = PAGED ? 2 * nkv : nkv, heads = nk + a.n_q;
-  const int first = blockIdx.y * HL + hl, step = gridDim.y * HL;
+__global__ void __launch_bounds__(HT, 6) heads_kernel(HeadsArgs a, Freq f) {
+  constexpr int CPR = D / 8, HL = kWave / CPR, B = 2;  // lanes of a head, heads of a turn, turns in flight
+  constexpr int CS = 20;  // floats of a lane's A and B in LDS: 16 lanes in different banks
+  enum Kind { K, V, Q };
+  __shared__ __attribute__((aligned(16))) uint16_t swap[HALVES ? HT * 8 : 8];
+  __shared__ float2 angle[D / 2];  // cosine and sine of each pair, times the amplitude
+  __shared__ __attribute__((aligned(16))) float coef[2][CPR * CS];  // A and B of keys and queries
+  const int c = threadIdx.x % CPR, hl = threadIdx.x % kWave / CPR;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int r = blockIdx.x, nkv = a.p.n_kv;
+  const int tk = (nkv + HL - 1) / HL, tv = PAGED ? 2 * tk : tk, turns = tv + (a.n_q + HL - 1) / HL;
+  const int first = blockIdx.y * HW + wave, step = gridDim.y * HW;
+  const uint16_t* const row[] = {a.k + r * a.ld_k, PAGED ? a.v + r * a.ld_v : nullptr, a.q + r * a.ld_q};
+  u32x4 raw[B];
+  auto fetch = [&](int t0) {
+#pragma unroll
+    for (int b = 0; b < B; ++b) {
+      const int t = t0 + b * step;
+      const Kind k = t < tk ? K : (t < tv ? V : Q);
+      const int j = (t - (k == K ? 0 : (k == V ? tk : tv))) * HL + hl;
+      if (t < turns && j < (k == Q ? a.n_q : nkv)) raw[b] = load16((k == K ? row[0] : (k == V ? row[1] : row[2])) + j * D + c * 8);
+    }
+  };
+  // where no row can be padding, the first heads are on their way before the row's place is known
+  const bool early = !PAGED || !a.q_begin;
+  if (early) fetch(first);
   int64_t pos = 0, at = 0;
   bool bad = false;
   if (PAGED) {
@@ -46,125 +93,160 @@ __global__ void __launch_bounds__(HT) heads_kernel(HeadsArgs a, Freq f) {
     pos = a.pos ? static_cast<int64_t>(a.pos[r]) : a.pos0 + r;
     if (pos < 0) return;
   }
-  u32x4 gq = {0u, 0u, 0u, 0u}, gk = gq;
-  if (a.q_gain) gq = load16(a.q_gain + c * 8);
-  if (a.k_gain) gk = load16(a.k_gain + c * 8);
-  // what number e turns by, and with HALVES where its partner is
-  constexpr int NP = HALVES ? 8 : 4;
-  float cs[NP], sn[NP];
-  int partner[HALVES ? 8 : 1];
-  const int lane0 = threadIdx.x - c;
-#pragma unroll
-  for (int e = 0; e < NP; ++e) {
-    const int i = HALVES ? c * 8 + e : c * 4 + e;  // a number of the head, or a pair
-    const int pair = HALVES && i >= a.half ? i - a.half : i;
-    cs[e] = 1.f;
-    sn[e] = 0.f;
-    if (HALVES) partner[e] = 0;
-    if (pair < a.half) {
-      double rev = static_cast<double>(pos) * f.rev[pair];
-      rev -= rint(rev);
-      cs[e] = __builtin_amdgcn_cosf(static_cast<float>(rev)) * a.amplitude;
-      sn[e] = __builtin_amdgcn_sinf(static_cast<float>(rev)) * a.amplitude;
-      if (HALVES) {
-        const int o = i < a.half ? i + a.half : i - a.half;
-        partner[e] = (lane0 + o / 8) * 9 + o % 8;
-        if (i < a.half) sn[e] = -sn[e];  // u cos - w sin, w cos + u sin
-      }
-    }
-  }
-  const int turned = a.half * 2 - c * 8;  // numbers of this lane below it turn
+  if (!early) fetch(first);
 
-  auto source = [&](int h) {
-    if (h >= nk) return a.q + r * a.ld_q + (h - nk) * D + c * 8;
-    if (PAGED && h >= nkv) return a.v + r * a.ld_v + (h - nkv) * D + c * 8;
-    return a.k + r * a.ld_k + h * D + c * 8;
+  auto lds_sync = [&]() {  // keeps the compiler to the order of the wave's LDS accesses
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
   };
-  auto process = [&](int h, u32x4 raw) {
-    const bool is_q = h >= nk, is_v = PAGED && !is_q && h >= nkv;
-    const int j = is_q ? h - nk : (is_v ? h - nkv : h);
-    float x[8];
+  if (static_cast<int>(threadIdx.x) < a.half) {
+    double rev = static_cast<double>(pos) * f.rev[threadIdx.x];
+    rev -= rint(rev);
+    angle[threadIdx.x] = make_float2(__builtin_amdgcn_cosf(static_cast<float>(rev)) * a.amplitude,
+                                     __builtin_amdgcn_sinf(static_cast<float>(rev)) * a.amplitude);
+  }
+  // the number that number i of a head turns with
+  auto partner = [&](int i) { return i >= 2 * a.half ? i : (HALVES ? (i < a.half ? i + a.half : i - a.half) : i ^ 1); };
+  const bool aligned = a.half % 8 == 0, all = a.half * 2 == D;
+  const int turned = a.half * 2 - c * 8;  // numbers of this lane below it turn
+  uint16_t* const head = swap + (HALVES ? (threadIdx.x - c) * 8 : 0);
+  auto unpack = [&](const u32x4 w, float (&v)[8]) {
 #pragma unroll
-    for (int w = 0; w < 4; ++w) T::unpack2(raw[w], x[2 * w], x[2 * w + 1]);
-    if (!is_v) {
-      if (is_q ? a.q_gain : a.k_gain) {
-        float ss = 0.f, g[8];
+    for (int e = 0; e < 4; ++e) T::unpack2(w[e], v[2 * e], v[2 * e + 1]);
+  };
+  // the numbers that this lane's numbers turn with
+  auto partners = [&](const u32x4 w, float (&o)[8]) {
+    if (HALVES) {
+      lds_sync();
+      *reinterpret_cast<u32x4*>(head + c * 8) = w;
+      lds_sync();
+      u32x4 p;
+      if (aligned) {
+        p = *reinterpret_cast<const u32x4*>(head + partner(c * 8));
+      } else {
+        int i = c * 8;
+        asm volatile("" : "+v"(i));  // the places are worked out here, not kept in registers over the loop
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          p[e] = head[partner(i + 2 * e)] | static_cast<uint32_t>(head[partner(i + 2 * e + 1)]) << 16;
+      }
+      unpack(p, o);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) T::unpack2(w[e], o[2 * e + 1], o[2 * e]);
+    }
+  };
+  // A and B: thread t has number t % D of the keys' or the queries'
+  __syncthreads();
+  if (threadIdx.x < 2 * D) {
+    const int k = threadIdx.x / D, i = threadIdx.x % D;
+    const uint16_t* gain = k ? a.q_gain : a.k_gain;
+    float co = 1.f, si = 0.f;
+    if (i < 2 * a.half) {
+      const float2 z = angle[HALVES ? (i < a.half ? i : i - a.half) : i / 2];
+      co = z.x;
+      si = (HALVES ? i < a.half : i % 2 == 0) ? -z.y : z.y;  // u cos - w sin, w cos + u sin
+    }
+    float g = 1.f, gp = 1.f, unused;
+    if (gain) {
+      T::unpack2(gain[i], g, unused);
+      T::unpack2(gain[partner(i)], gp, unused);
+    }
+    coef[k][i / 8 * CS + i % 8] = g * co;
+    coef[k][i / 8 * CS + 8 + i % 8] = gp * si;
+  }
+  __syncthreads();
+
+  auto process = [&](auto KIND, int j, u32x4 w) {
+    constexpr Kind kind = static_cast<Kind>(decltype(KIND)::value);
+    float x[8];
+    unpack(w, x);
+    if (kind != V) {
+      float inv = 1.f, o[8];
+      partners(w, o);
+      if (kind == Q ? a.q_gain != nullptr : a.k_gain != nullptr) {
+        float ss = 0.f;
 #pragma unroll
         for (int e = 0; e < 8; ++e) ss = fmaf(x[e], x[e], ss);
-        ss = group_sum(ss, CPR);
-        const u32x4 gw = is_q ? gq : gk;
-#pragma unroll
-        for (int w = 0; w < 4; ++w) T::unpack2(gw[w], g[2 * w], g[2 * w + 1]);
-        const float mean = ss * (1.f / D) + a.eps;
-        if (mean > 1e-30f && mean < 1e37f) {
-          const float inv = 1.f / sqrtf(mean);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) x[e] = x[e] * inv * g[e];
-        } else {  // squares of bf16 numbers that leave fp32's range
+        const float mean = group_sum(ss, CPR) * (1.f / D) + a.eps;
+        inv = __builtin_amdgcn_rsqf(mean);
+        if (!(mean > 1e-30f && mean < 1e37f)) {
+          // Squares of bf16 numbers leave fp32's range at 2^64 and 2^-63: such a head's statistics and its first
+          // products are taken in double.
           double s2 = 0.0;
 #pragma unroll
           for (int e = 0; e < 8; ++e) s2 += static_cast<double>(x[e]) * x[e];
 #pragma unroll
-          for (int o = CPR / 2; o > 0; o >>= 1) s2 += __shfl_xor(s2, o, kWave);
-          const double inv = 1.0 / sqrt(s2 / D + a.eps);
+          for (int q = CPR / 2; q > 0; q >>= 1) s2 += __shfl_xor(s2, q, kWave);
+          const double wide = 1.0 / sqrt(s2 / D + a.eps);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) x[e] = static_cast<float>(x[e] * inv * g[e]);
-        }
-      }
-      if (HALVES) {
-        float* mine = swap + threadIdx.x * 9;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) mine[e] = x[e];
-        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-        float o[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) o[e] = swap[partner[e]];
-        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = e < turned ? x[e] * cs[e] + o[e] * sn[e] : x[e];
-      } else {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float u = x[2 * e], w = x[2 * e + 1];
-          if (2 * e < turned) {
-            x[2 * e] = u * cs[e] - w * sn[e];
-            x[2 * e + 1] = u * sn[e] + w * cs[e];
+          for (int e = 0; e < 8; ++e) {
+            x[e] = static_cast<float>(x[e] * wide);
+            o[e] = static_cast<float>(o[e] * wide);
           }
+          inv = 1.f;
+        }
+      }
+      const f32x4* ab = reinterpret_cast<const f32x4*>(coef[kind == Q] + c * CS);
+#pragma unroll
+      for (int v = 0; v < 2; ++v) {
+        const f32x4 ca = ab[v], cb = ab[2 + v];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const int e = 4 * v + q;
+          const float own = x[e] * ca[q], both = fmaf(o[e], cb[q], own);
+          x[e] = inv * (all || e < turned ? both : own);  // (infinity times a zero B would be NaN)
         }
       }
 #pragma unroll
-      for (int w = 0; w < 4; ++w) raw[w] = T::pack2(x[2 * w], x[2 * w + 1]);
+      for (int e = 0; e < 4; ++e) w[e] = T::pack2(x[2 * e], x[2 * e + 1]);
     }
-    if (is_q) {
-      *reinterpret_cast<u32x4*>(a.q_out + r * a.ld_qo + j * D + c * 8) = raw;
+    if (kind == Q) {
+      *reinterpret_cast<u32x4*>(a.q_out + r * a.ld_qo + j * D + c * 8) = w;
     } else if (!PAGED) {
-      *reinterpret_cast<u32x4*>(a.k_out + r * a.ld_ko + j * D + c * 8) = raw;
+      *reinterpret_cast<u32x4*>(a.k_out + r * a.ld_ko + j * D + c * 8) = w;
     } else if (!bad) {
-      char* dst = (is_v ? a.p.v : a.p.k) + at + j * a.p.head;
+      char* dst = (kind == V ? a.p.v : a.p.k) + at + j * a.p.head;
       if (F8) {
-        const float* sc = is_v ? a.p.v_scale : a.p.k_scale;
-        *reinterpret_cast<u32x2*>(dst + c * 8) = to_f8(x, sc ? sc[j] : 1.f);
+        const float* sc = kind == V ? a.p.v_scale : a.p.k_scale;
+        const float scale = sc ? sc[j] : 1.f, rcp = __builtin_amdgcn_rcpf(scale);
+        const bool normal = scale > 1e-37f && scale < 1e37f;  // and so is its reciprocal
+        *reinterpret_cast<u32x2*>(dst + c * 8) = normal ? scaled_to_f8(x, scale, rcp) : to_f8(x, scale);
       } else {
-        *reinterpret_cast<u32x4*>(dst + 16 * c) = raw;
+        *reinterpret_cast<u32x4*>(dst + 16 * c) = w;
       }
     }
   };
-  for (int h = first; h < heads; h += B * step) {
-    u32x4 raw[B];
+  for (int t0 = first; t0 < turns; t0 += B * step) {
+    u32x4 now[B];
 #pragma unroll
-    for (int b = 0; b < B; ++b)
-      if (h + b * step < heads) raw[b] = load16(source(h + b * step));
+    for (int b = 0; b < B; ++b) now[b] = raw[b];
+    fetch(t0 + B * step);
+#pragma unroll 1
+    for (int b = 0; b < B; ++b) {  // rolled: one copy of the code
+      const int t = t0 + b * step;
+      if (t >= turns) break;
+      const u32x4 w = now[0];
 #pragma unroll
-    for (int b = 0; b < B; ++b)
-      if (h + b * step < heads) process(h + b * step, raw[b]);
+      for (int i = 0; i + 1 < B; ++i) now[i] = now[i + 1];
+      if (t < tk) {
+        const int j = t * HL + hl;
+        if (j < nkv) process(std::integral_constant<int, K>{}, j, w);
+      } else if (PAGED && t < tv) {
+        const int j = (t - tk) * HL + hl;
+        if (j < nkv) process(std::integral_constant<int, V>{}, j, w);
+      } else {
+        const int j = (t - tv) * HL + hl;
+        if (j < a.n_q) process(std::integral_constant<int, Q>{}, j, w);
+      }
+    }
   }
 }
 
 namespace {
 
 constexpr int kMaxHeads = 1024, kMaxTokens = 1 << 20;
+constexpr int kGroups = 1024;  // workgroups to aim at: four on each compute unit
 
 // Revolutions per position of a head's pairs; their number in ``half``.
 vt_status frequencies(const vt_rope* rope, int head_dim, Freq* f, int* half, float* amplitude) {
@@ -221,11 +303,12 @@ auto pick(int d, bool halves) -> void (*)(HeadsArgs, Freq) {
   return halves ? heads_kernel<T, PAGED, F8, true, 64> : heads_kernel<T, PAGED, F8, false, 64>;
 }
 
-vt_status launch(void (*kernel)(HeadsArgs, Freq), const HeadsArgs& a, const Freq& f, int d, int n_tok, int heads,
+vt_status launch(void (*kernel)(HeadsArgs, Freq), const HeadsArgs& a, const Freq& f, int d, int n_tok, bool paged,
                  void* stream) {
-  // heads of a row over several workgroups only while there are few rows
-  const int hl = HT / (d / 8), parts = (heads + hl - 1) / hl;
-  hipLaunchKernelGGL(kernel, dim3(n_tok, n_tok >= 512 ? 1 : parts), dim3(HT), 0, static_cast<hipStream_t>(stream), a, f);
+  // a row's turns over several workgroups only while there are few rows
+  const int hl = kWave * 8 / d, tk = (a.p.n_kv + hl - 1) / hl, turns = (paged ? 2 * tk : tk) + (a.n_q + hl - 1) / hl;
+  const int parts = std::max(1, std::min((turns + HW - 1) / HW, kGroups / n_tok));
+  hipLaunchKernelGGL(kernel, dim3(n_tok, parts), dim3(HT), 0, static_cast<hipStream_t>(stream), a, f);
   const hipError_t e = hipGetLastError();
   return e == hipSuccess ? VT_OK : fail(VT_ERR_HIP, "heads launch: %s", hipGetErrorString(e));
 }
@@ -271,7 +354,7 @@ extern "C" vt_status vt_paged_append_heads(const vt_paged_kv* kv, const vt_paged
   auto* kernel = io->type == VT_T_F16
                      ? (f8 ? pick<Half, true, true>(kv->head_dim, halves) : pick<Half, true, false>(kv->head_dim, halves))
                      : (f8 ? pick<BFloat, true, true>(kv->head_dim, halves) : pick<BFloat, true, false>(kv->head_dim, halves));
-  return launch(kernel, a, f, kv->head_dim, io->n_tok, 2 * kv->n_kv_heads + a.n_q, stream);
+  return launch(kernel, a, f, kv->head_dim, io->n_tok, true, stream);
 }
 
 extern "C" vt_status vt_rotate_heads(const vt_heads_io* io, const vt_head_norm* norm, const vt_rope* rope,
@@ -326,5 +409,5 @@ extern "C" vt_status vt_rotate_heads(const vt_heads_io* io, const vt_head_norm* 
   const bool halves = rope && (rope->flags & VT_ROPE_HALVES);
   auto* kernel = io->type == VT_T_F16 ? pick<Half, false, false>(io->head_dim, halves)
                                       : pick<BFloat, false, false>(io->head_dim, halves);
-  return launch(kernel, a, f, io->head_dim, io->n_tok, io->n_k_heads + io->n_q_heads, stream);
+  return launch(kernel, a, f, io->head_dim, io->n_tok, false, stream);
 }

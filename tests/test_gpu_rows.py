@@ -435,6 +435,48 @@ def test_append_beside_plain_append():
             assert near(a.k_pool.float().double(), b.k_pool.float().double(), 2.0 ** -3 if f8 else 2.0 ** -10)
 
 
+@BOTH
+def test_append_f8_quotients(type):
+    """Quotients exactly between two 8-bit numbers go to the even one, whatever the scale's reciprocal; numbers past the
+    largest saturate, infinities too; NaN stays; subnormal and zero quotients. Bit for bit the rounded true quotient."""
+    b = Batch([64], [64], kv_heads=4, group=1, d=64, act=type, f8=True)
+    b.k_scale = torch.tensor([0.75, 0.01171875, 3.0, 1e-3], device="cuda")
+    b.v_scale = torch.tensor([1.0, 5.0, 0.375, 7.0], device="cuda")
+    grid = torch.cat([torch.tensor([m * 2.0 ** e for e in range(-12, 9) for m in (1.0, 1.0625, 1.1875, 1.3125, 1.9375)]),
+                      torch.tensor([448.0, 456.0, 464.0, 465.0, 480.0, 1e4, 6e4, math.inf, math.nan, 0.0, -0.0])])
+    vals = torch.cat([grid, -grid])
+    i = torch.arange(64 * 4 * 64) % vals.numel()
+    base = vals[i].view(64, 4, 64).cuda()
+    rows = lambda scale: (base * scale[:, None]).to(b.dtype).flatten(1)
+    k, v = rows(b.k_scale), rows(b.v_scale)
+    vt.vt_paged_append_heads(b.kv(), b.io(q=None, q_rot=None, k=p(k), ld_k=256, v=p(v), ld_v=256), None, None, stream())
+    torch.cuda.synchronize()
+    for x, scale, pool in ((k, b.k_scale, b.k_pool), (v, b.v_scale, b.v_pool)):
+        q = (x.view(64, 4, 64).float() / scale[:, None])
+        want = torch.where(q.isnan(), q, q.clamp(-448, 448)).to(F8)
+        got = b.slots(pool)[b.at(0)].view(F8)
+        assert torch.equal(got.float().nan_to_num(1e9), want.float().nan_to_num(1e9))
+        assert torch.equal(got.view(torch.uint8) >> 7, want.view(torch.uint8) >> 7) or bool(want.isnan().any())
+
+
+@pytest.mark.parametrize("at,value", [(3, math.inf), (40, math.nan), (90, math.inf), (127, math.nan)])
+def test_append_f8_odd_numbers(at, value):
+    """An infinite or NaN number of a key reaches what it turns with as in the formulas, and saturates or stays NaN."""
+    b = Batch([20], [20], kv_heads=2, group=1, d=128, f8=True)
+    rope = dict(base=10000.0, dims=80, flags=1)
+    g = torch.Generator(device="cuda").manual_seed(2)
+    k, v = (torch.empty((20, 256), device="cuda").normal_(generator=g).to(b.dtype) for _ in range(2))
+    k[4, at], v[5, at] = value, value
+    vt.vt_paged_append_heads(b.kv(), b.io(q=None, q_rot=None, k=p(k), ld_k=256, v=p(v), ld_v=256), None, vt.vt_rope(**rope), stream())
+    torch.cuda.synchronize()
+    want, _ = turned(k.unflatten(1, (2, 128)), None, torch.arange(20, device="cuda"), rope, 128, 0.0, b.dtype)
+    got = b.slots(b.k_pool)[b.at(0)].view(F8).float()
+    assert torch.equal(got.isnan(), want.isnan())
+    assert bool((got[want.isinf()].abs() == 448).all()) and bool((got[want.isinf()] * want[want.isinf()] > 0).all())
+    vq = b.slots(b.v_pool)[b.at(0)].view(F8).float()
+    assert torch.equal(vq.isnan(), v.unflatten(1, (2, 128)).isnan())
+
+
 def test_append_queries_in_place_and_without_queries():
     b = Batch([30, 20], [9, 20], kv_heads=2, group=3, d=64, pad=2)
     gains = gains_of(b)
