@@ -54,46 +54,86 @@ constexpr Cost kMidCost[] = {{3.439, 0.1371, 0.151, 0.0975, 0.0, 1.111, 0.427, 0
                              {2.863, 0.1901, 0.825, 0.0530, 0.00912, 1.480, 0.266, 0.136},
                              {1.706, 0.2589, 2.297, 0.0731, 0.01407, 2.096, 0.260, 0.240},
                              {1.794, 0.4144, 3.204, 0.0268, 0.02384, 2.011, 0.182, 0.583}};
-constexpr Cost kTileCost[] = {{3.620, 0.5503, 5.360, 0.0649, 0.02155, 0, 0, 0},
-                              {5.131, 0.9108, 9.962, 0.0434, 0.02568, 0, 0, 0}};
+constexpr Cost kNarrowCost = {3.620, 0.5503, 5.360, 0.0649, 0.02155, 0, 0, 0};
+constexpr Cost kWideCost = {5.131, 0.9108, 9.962, 0.0434, 0.02568, 0, 0, 0};
 constexpr int kSlices[] = {1, 2, 3, 4, 6, 8, 12, 16};
 constexpr int kThinRows = 16;  // beyond, the thin tile reads the weights more than once
+constexpr int kUnits = 256;    // compute units
+
+enum Kernel { kUseThin, kUseMid, kUseTile };
 
 struct Plan {
-  int kernel;  // -1: thin, then those of kMid, then of kTile
-  int m_tiles, n_tiles, splits, steps;
+  Kernel kernel;
+  int mid;     // of kMid
+  int m_tiles, n_tiles, wide, splits, steps;
   double us;
 };
+
+int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// The last compute unit's end where ``many`` tiles of cost c start first and ``more`` of cost d fill up.
+double ends_at(int64_t many, double c, int64_t more, double d) {
+  const int64_t all = many / kUnits, odd = many % kUnits;  // odd units take one more of the first
+  double end = static_cast<double>(all + (odd ? 1 : 0)) * c;
+  for (int64_t n = up(more, kUnits);; ++n) {  // a unit takes up to n of the others
+    const double t = std::max(end, all * c + n * d);
+    const int64_t busy = odd ? static_cast<int64_t>((t - (all + 1) * c) / d) : 0;
+    if ((kUnits - odd) * static_cast<int64_t>((t - all * c) / d + 1e-9) + odd * busy >= more) return t;
+  }
+}
 
 Plan plan_of(int64_t M, int64_t N, int64_t K, bool gated) {
   Plan best{};
   best.us = std::numeric_limits<double>::infinity();
-  const int64_t all = (K + 63) / 64;
+  const int64_t all = up(K, 64);
   const double mb = 2e-6 * (static_cast<double>(N) * K * (gated ? 2 : 1) + static_cast<double>(M) * (K + N));
-  auto consider = [&](int kernel, lin::Shape shape, const Cost& c, bool split) {
-    const bool thin = kernel < 0;
+  auto consider = [&](Kernel kernel, int mid, lin::Shape shape, const Cost& c) {
+    const bool thin = kernel == kUseThin;
     const int64_t out = gated && !thin ? shape.features / 2 : shape.features;
     const int64_t wrows = gated && thin ? 2 * shape.features : shape.features;  // weight rows of a tile
-    const int64_t mt = (M + shape.rows - 1) / shape.rows, nt = (N + out - 1) / out, tiles = mt * nt;
+    const int64_t mt = up(M, shape.rows), nt = up(N, out), tiles = mt * nt;
     int64_t last = 0;
     for (int want : kSlices) {
-      if (want > 1 && (!split || tiles > lin::kMaxTiles)) break;
-      const int64_t steps = (all + want - 1) / want, splits = (all + steps - 1) / steps, work = tiles * splits;
+      if (want > 1 && (tiles > lin::kMaxTiles || tiles * want > 6 * kUnits || all < 2 * want)) break;
+      const int64_t steps = up(all, want), splits = up(all, steps), work = tiles * splits;
       const int64_t part = splits > 1 ? 4 * work * shape.rows * wrows : 0;
       if (splits == last || part > static_cast<int64_t>(lin::kPartBytes)) continue;
       last = splits;
-      const double rounds = static_cast<double>((work + 255) / 256);
+      const double rounds = static_cast<double>(up(work, kUnits));
       const double loads = 128e-6 * static_cast<double>(work) * steps * (shape.rows + wrows);
       const double us = c.start + rounds * (c.step * steps + c.tile) + c.memory * mb + c.l2 * loads +
                         (splits > 1 ? c.join + c.part * 1e-6 * part + c.slice * splits : 0.0);
       if (us < best.us)
-        best = {kernel, static_cast<int>(mt), static_cast<int>(nt), static_cast<int>(splits), static_cast<int>(steps), us};
+        best = {kernel,  mid, static_cast<int>(mt), static_cast<int>(nt), 0, static_cast<int>(splits), static_cast<int>(steps), us};
     }
   };
-  if (M <= kThinRows) consider(-1, lin::kThin, kThinCost, true);
-  int kernel = 0;
-  for (size_t i = 0; i < std::size(lin::kMid); ++i) consider(kernel++, lin::kMid[i], kMidCost[i], true);
-  for (size_t i = 0; i < std::size(lin::kTile); ++i) consider(kernel++, lin::kTile[i], kTileCost[i], false);
+  if (M <= kThinRows) consider(kUseThin, 0, lin::kThin, kThinCost);
+  for (size_t i = 0; i < std::size(lin::kMid); ++i)
+    if (lin::kMid[i].rows <= 64 || lin::kMid[i].rows < 4 * M)  // the others only multiply more rows that are not there
+      consider(kUseMid, static_cast<int>(i), lin::kMid[i], kMidCost[i]);
+  if (M > 64) {
+    // Wide tiles, as many whole rounds of them as there are or some fewer, and narrow ones for the rest.
+    const int64_t mt = up(M, lin::kWide.rows), wide = lin::kWide.features / (gated ? 2 : 1), narrow = wide / 2;
+    const int64_t cols = up(N, wide);
+    auto tile = [&](int64_t w) {
+      const int64_t n = N > w * wide ? up(N - w * wide, narrow) : 0;
+      const Cost& c = w ? kWideCost : kNarrowCost;
+      const double loads = 128e-6 * static_cast<double>(all * mt) *
+                           (w * (lin::kWide.rows + lin::kWide.features) + n * (lin::kNarrow.rows + lin::kNarrow.features));
+      const double us = c.start + ends_at(w * mt, kWideCost.step * all + kWideCost.tile, n * mt,
+                                          kNarrowCost.step * all + kNarrowCost.tile) +
+                        c.memory * mb + c.l2 * loads;
+      if (us < best.us)
+        best = {kUseTile, 0, static_cast<int>(mt), static_cast<int>(n), static_cast<int>(w), 1, static_cast<int>(all), us};
+    };
+    tile(0);
+    tile(cols);
+    const int64_t rounds = cols * mt / kUnits;
+    for (int64_t r = std::max<int64_t>(1, rounds - 2); r <= rounds; ++r) {
+      const int64_t w = std::min(cols, r * kUnits / mt);
+      if (w > 0 && w < cols) tile(w);
+    }
+  }
   return best;
 }
 
@@ -139,18 +179,18 @@ vt_status project(const vt_linear_io* io, bool gated, void* ws, size_t ws_bytes,
   const Plan p = plan_of(a.M, a.N, a.K, gated);
   a.m_tiles = p.m_tiles;
   a.n_tiles = p.n_tiles;
+  a.wide = p.wide;
   a.splits = p.splits;
   a.steps = p.steps;
   a.arrived = static_cast<uint32_t*>(ws);
   a.part = reinterpret_cast<float*>(static_cast<char*>(ws) + lin::kSyncBytes);
-  if (lin::grid_of(p.m_tiles, static_cast<int64_t>(p.n_tiles) * p.splits) >= (int64_t(1) << 23))  // 2^32 threads
-    return fail(VT_ERR_UNSUPPORTED, "%d x %d tiles: fewer rows or features per call", p.m_tiles, p.n_tiles);
+  if (lin::grid_of(p.m_tiles, static_cast<int64_t>(p.n_tiles) * p.splits) + lin::grid_of(p.m_tiles, p.wide) >= (int64_t(1) << 22))
+    return fail(VT_ERR_UNSUPPORTED, "%d x %d tiles: fewer rows or features per call", p.m_tiles, p.n_tiles + p.wide);
   const bool bf16 = io->type == VT_T_BF16;
   const hipStream_t s = static_cast<hipStream_t>(stream);
-  constexpr int mids = static_cast<int>(std::size(lin::kMid));
-  const hipError_t e = p.kernel < 0      ? lin::launch_thin(a, bf16, gated, s)
-                       : p.kernel < mids ? lin::launch_mid(a, p.kernel, bf16, gated, s)
-                                         : lin::launch_tile(a, p.kernel > mids, bf16, gated, s);
+  const hipError_t e = p.kernel == kUseThin  ? lin::launch_thin(a, bf16, gated, s)
+                       : p.kernel == kUseMid ? lin::launch_mid(a, p.mid, bf16, gated, s)
+                                             : lin::launch_tile(a, bf16, gated, s);
   return e == hipSuccess ? VT_OK : fail(VT_ERR_HIP, "projection launch: %s", hipGetErrorString(e));
 }
 

@@ -26,6 +26,7 @@ struct Args {
   int64_t ld_x, ld_w[2], ld_r, ld_y;
   int32_t M, N, K, act;
   int32_t m_tiles, n_tiles;
+  int32_t wide;           // tile kernel: columns of 256 weight rows before the n_tiles of 128
   int32_t splits, steps;  // slices of K, and the k-steps of each
   float* part;            // the slices' sums
   uint32_t* arrived;      // per tile: slices done, zero between calls
@@ -40,9 +41,9 @@ constexpr size_t kPartBytes = size_t(64) << 20;
 // one; each XCD gets one run of the tiles in the order of blocks of 2048 rows, column by column in them, so
 // that the tiles running there at once share rows and weights in its L2. False: a workgroup too many.
 constexpr int kXcds = 8;
-inline int64_t grid_of(int64_t m_tiles, int64_t cols) { return (m_tiles * cols + kXcds - 1) / kXcds * kXcds; }
-__device__ __forceinline__ bool my_tile(int m_tiles, int cols, int tile_rows, int& m, int& col) {
-  const int all = m_tiles * cols, run = (all + kXcds - 1) / kXcds, id = blockIdx.x;
+__host__ __device__ inline int64_t grid_of(int64_t m_tiles, int64_t cols) { return (m_tiles * cols + kXcds - 1) / kXcds * kXcds; }
+__device__ __forceinline__ bool my_tile(int id, int m_tiles, int cols, int tile_rows, int& m, int& col) {
+  const int all = m_tiles * cols, run = (all + kXcds - 1) / kXcds;
   const int at = id % kXcds * run + id / kXcds;
   if (at >= all) return false;
   const int high = min(m_tiles, max(1, 2048 / tile_rows)), blk = at / (high * cols);
@@ -184,7 +185,7 @@ struct Shape {
 };
 constexpr Shape kThin = {16, 16};
 constexpr Shape kMid[] = {{16, 64}, {32, 64}, {64, 64}, {64, 128}, {128, 128}};
-constexpr Shape kTile[] = {{256, 128}, {256, 256}};
+constexpr Shape kNarrow = {256, 128}, kWide = {256, 256};
 
 // Dynamic LDS above 64 KiB has to be asked for, kernel by kernel, once per device.
 class LdsOnce {
@@ -206,8 +207,8 @@ class LdsOnce {
 };
 
 hipError_t launch_thin(const Args& a, bool bf16, bool gated, hipStream_t s);
-hipError_t launch_mid(const Args& a, int which, bool bf16, bool gated, hipStream_t s);   // of kMid
-hipError_t launch_tile(const Args& a, bool wide, bool bf16, bool gated, hipStream_t s);  // of kTile
+hipError_t launch_mid(const Args& a, int which, bool bf16, bool gated, hipStream_t s);  // of kMid
+hipError_t launch_tile(const Args& a, bool bf16, bool gated, hipStream_t s);
 
 }  // namespace lin
 }  // namespace vt

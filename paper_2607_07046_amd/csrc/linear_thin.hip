@@ -23,7 +23,7 @@ __global__ void __launch_bounds__(NW* kWave) thin_kernel(Args a) {
   __shared__ __attribute__((aligned(16))) float red[HW * TM * LD];
   __shared__ uint32_t ticket;
   int m_tile, unit;
-  if (!my_tile(a.m_tiles, a.n_tiles * a.splits, TM, m_tile, unit)) return;
+  if (!my_tile(blockIdx.x, a.m_tiles, a.n_tiles * a.splits, TM, m_tile, unit)) return;
   const int n_tile = unit % a.n_tiles, split = unit / a.n_tiles;
   const int m0 = m_tile * TM, n0 = n_tile * TN;
   const int t = threadIdx.x, lane = t % kWave, wave = __builtin_amdgcn_readfirstlane(t / kWave);

@@ -28,16 +28,13 @@ constexpr int tile_lds(int mb, int nb) {
   return ring > epilogue ? ring : epilogue;
 }
 
-// MB, NB: 16-row blocks of rows and of weights of a wave.
+// The tile of row m_tile and of the features from n0. MB, NB: 16-row blocks of rows and of weights of a wave.
 template <class T, bool GATED, int MB, int NB>
-__global__ void __launch_bounds__(TT, 1) tile_kernel(Args a) {
-  extern __shared__ __attribute__((aligned(16))) char lds[];
+__device__ __forceinline__ void tile(const Args& a, char* lds, int m_tile, int n0) {
   constexpr int SLOT = slot_bytes(MB, NB), XB = 2 * MB * 1024;
   constexpr int TM = 32 * MB, TN = 32 * NB, NO = GATED ? TN / 2 : TN;  // rows, weight rows, features of a tile
   constexpr int P = MB * NB, R = MB + NB, LX = MB / 2, LPS = R / 2;    // products, reads, loads of a wave per half
-  int m_tile, n_tile;
-  if (!my_tile(a.m_tiles, a.n_tiles, TM, m_tile, n_tile)) return;
-  const int m0 = m_tile * TM, n0 = n_tile * NO;
+  const int m0 = m_tile * TM;
   const int t = threadIdx.x, lane = t % kWave, wave = __builtin_amdgcn_readfirstlane(t / kWave);
   const int full = a.K / TK;
   const bool tail = full * TK < a.K;
@@ -282,21 +279,33 @@ __global__ void __launch_bounds__(TT, 1) tile_kernel(Args a) {
   });
 }
 
-hipError_t launch_tile(const Args& a, bool wide, bool bf16, bool gated, hipStream_t s) {
+// Columns of wide tiles, then of narrow ones, which fill the last round of the compute units.
+template <class T, bool GATED>
+__global__ void __launch_bounds__(TT, 1) tile_kernel(Args a) {
+  extern __shared__ __attribute__((aligned(16))) char lds[];
+  constexpr int WIDE = kWide.features / (GATED ? 2 : 1), NARROW = kNarrow.features / (GATED ? 2 : 1);
+  const int id = blockIdx.x, wide = static_cast<int>(grid_of(a.m_tiles, a.wide));
+  int m, col;
+  if (id < wide) {
+    if (my_tile(id, a.m_tiles, a.wide, kWide.rows, m, col)) tile<T, GATED, 8, 8>(a, lds, m, col * WIDE);
+  } else {
+    if (my_tile(id - wide, a.m_tiles, a.n_tiles, kNarrow.rows, m, col))
+      tile<T, GATED, 8, 4>(a, lds, m, a.wide * WIDE + col * NARROW);
+  }
+}
+
+hipError_t launch_tile(const Args& a, bool bf16, bool gated, hipStream_t s) {
   static LdsOnce once;
-  void (*const kernels[2][4])(Args) = {
-      {tile_kernel<Half, false, 8, 4>, tile_kernel<Half, true, 8, 4>, tile_kernel<BFloat, false, 8, 4>,
-       tile_kernel<BFloat, true, 8, 4>},
-      {tile_kernel<Half, false, 8, 8>, tile_kernel<Half, true, 8, 8>, tile_kernel<BFloat, false, 8, 8>,
-       tile_kernel<BFloat, true, 8, 8>}};
-  const int lds[] = {tile_lds(8, 4), tile_lds(8, 8)};
+  void (*const kernels[])(Args) = {tile_kernel<Half, false>, tile_kernel<Half, true>, tile_kernel<BFloat, false>,
+                                   tile_kernel<BFloat, true>};
+  constexpr int lds = tile_lds(8, 8) > tile_lds(8, 4) ? tile_lds(8, 8) : tile_lds(8, 4);
+  static_assert(lds <= 160 * 1024, "one workgroup per compute unit");
   const hipError_t e = once([&](auto&& raise) {
-    for (int w = 0; w < 2; ++w)
-      for (auto* f : kernels[w]) raise(reinterpret_cast<const void*>(f), lds[w]);
+    for (auto* f : kernels) raise(reinterpret_cast<const void*>(f), lds);
   });
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(kernels[wide][2 * bf16 + gated], dim3(static_cast<uint32_t>(grid_of(a.m_tiles, a.n_tiles))),
-                     dim3(TT), lds[wide], s, a);
+  const int64_t grid = grid_of(a.m_tiles, a.wide) + grid_of(a.m_tiles, a.n_tiles);
+  hipLaunchKernelGGL(kernels[2 * bf16 + gated], dim3(static_cast<uint32_t>(grid)), dim3(TT), lds, s, a);
   return hipGetLastError();
 }
 

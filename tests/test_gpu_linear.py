@@ -29,7 +29,9 @@ SHAPES = [(1, 1, 1), (1, 7, 5), (1, 8, 16), (1, 64, 17), (1, 65, 16), (1, 512, 1
 LARGE = [(20, 898, 75), (2279, 1322, 9), (754, 1846, 30), (1089, 2307, 21), (2885, 130, 140), (2794, 2496, 30),
          (3119, 2210, 17), (262, 37, 1836), (1577, 33, 673), (614, 3771, 769), (2575, 3719, 196), (663, 33, 3138),
          (781, 100, 2565), (337, 4092, 2839), (90, 8193, 4141), (80, 5742, 3326), (1378, 256, 3918), (2171, 230, 2423),
-         (2337, 65, 2682), (3785, 33, 4161), (4115, 200, 3319), (3380, 1, 3699), (3869, 359, 3362), (2500, 448, 4008)]
+         (2337, 65, 2682), (3785, 33, 4161), (4115, 200, 3319), (3380, 1, 3699), (3869, 359, 3362), (2500, 448, 4008),
+         (862, 256, 5974), (1249, 1, 4901), (1420, 1, 8586), (2774, 64, 4459), (3939, 75, 5250), (3887, 1, 3044),
+         (2046, 64, 5268)]
 SHAPES += LARGE
 
 
