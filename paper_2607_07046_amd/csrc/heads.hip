@@ -6,11 +6,10 @@
 #include <cmath>
 #include <type_traits>
 
-#include "paged.hpp"
+#include "paged_append.hpp"
 
 namespace vt {
 namespace pg {
-
 
 constexpr int HT = 256, HW = HT / kWave;  // threads and waves per workgroup
 

@@ -14,6 +14,15 @@
 //
 // Rows past the matrices' ends are read from their last row (the sums are never stored). The stage that reaches
 // past K goes through registers, masked, and is multiplied first.
+//
+// What bounds it: up to about 64 rows reading the weights, above it LDS (at 128 x 128 its reads and the loads' writes take
+// 768 cycles of a stage, the products 512). Measured in bf16: 64 rows of 8192 through the gate and up projections of
+// 7168 features 48 to 55 us, 4.3 to 4.9 TB/s; rows of 4096 through 4096 features: 256 rows 18 us (474 TFLOP/s),
+// 512 25 (676), 1024 40 (853); 777 rows of 3302 to 4096 with a residual 39 to 43, 30 at 3328. Rows that do not start at
+// 128-byte lines cost that: half of each line is fetched again for the next stage. Tried for them and not kept, since
+// each lost more elsewhere: whole lines into LDS and fragments from two stages (64 rows through 14336 features 32
+// us, not 39, but 20 to 60% slower wherever the weights were in the caches), and two stages' loads together (777 rows 38,
+// not 42, other sizes 2 to 15% slower). 64 x 64 per wave on the large tile's schedule: 0 to 8% faster than 128 x 128 here.
 #include "linear_lds.hpp"
 
 namespace vt {

@@ -5,7 +5,7 @@
 #include <algorithm>
 #include <cmath>
 
-#include "paged.hpp"
+#include "paged_append.hpp"
 
 namespace vt {
 namespace pg {

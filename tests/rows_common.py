@@ -25,17 +25,21 @@ def least(dtype):
     return float(torch.finfo(dtype).smallest_normal) * torch.finfo(dtype).eps / 2
 
 
-def matrix(g, rows, cols, dtype, pad=8, sigma=1.0, fill=math.nan):
-    """[rows][cols] of a wider buffer whose other numbers are ``fill``."""
-    ld = -(-cols // 8) * 8 + pad
-    t = torch.full((rows, ld), fill, dtype=dtype, device="cuda")
+def stride_of(cols, pad):
+    """A row stride; pad "lines": of whole 128-byte lines."""
+    return -(-cols // 64) * 64 if pad == "lines" else -(-cols // 8) * 8 + pad
+
+
+def matrix(g, rows, cols, dtype, pad=8, sigma=1.0, fill=math.nan, shift=0):
+    """[rows][cols] of a wider buffer whose other numbers are ``fill``, ``shift`` numbers behind its start."""
+    ld = stride_of(cols, pad)
+    t = torch.full((rows * ld + shift,), fill, dtype=dtype, device="cuda")[shift:].view(rows, ld)
     t[:, :cols] = torch.empty((rows, cols), device="cuda").normal_(0, sigma, generator=g).to(dtype)
     return t[:, :cols]
 
 
 def marked(rows, cols, dtype, pad=8):
-    ld = -(-cols // 8) * 8 + pad
-    return torch.full((rows, ld), MARK, dtype=dtype, device="cuda")[:, :cols]
+    return torch.full((rows, stride_of(cols, pad)), MARK, dtype=dtype, device="cuda")[:, :cols]
 
 
 def around(t):
@@ -75,13 +79,13 @@ class Linear:
     """One projection: operands on the device, the call, the definition."""
 
     def __init__(self, type, M, K, N, act="none", bias=False, residual=False, gated=False, pad=8, seed=0, sigma=1.0,
-                 positive=False):
+                 positive=False, shift=0):
         g = torch.Generator(device="cuda").manual_seed(seed)
         self.dtype, self.type = ACT_TYPES[type]
         self.M, self.K, self.N, self.act, self.gated = M, K, N, act, gated
-        self.x = matrix(g, M, K, self.dtype, pad, sigma)
-        self.w = matrix(g, N, K, self.dtype, pad, K ** -0.5)
-        self.w_up = matrix(g, N, K, self.dtype, pad, K ** -0.5) if gated else None
+        self.x = matrix(g, M, K, self.dtype, pad, sigma, shift=shift)
+        self.w = matrix(g, N, K, self.dtype, pad, K ** -0.5, shift=shift)
+        self.w_up = matrix(g, N, K, self.dtype, 24 if pad == 8 else pad, K ** -0.5) if gated else None
         if positive:  # sums that only grow
             for t in (self.x, self.w):
                 t.abs_()

@@ -35,18 +35,24 @@ LARGE = [(20, 898, 75), (2279, 1322, 9), (754, 1846, 30), (1089, 2307, 21), (288
 SHAPES += LARGE
 
 
+# rows between 128-byte lines, at them, and matrices that start between them
+PLACES = pytest.mark.parametrize("pad,shift", [(8, 0), ("lines", 0), ("lines", 40), (16, 8)])
+
+
 @BOTH
+@PLACES
 @pytest.mark.parametrize("M,K,N", SHAPES)
-def test_shapes(ws, type, M, K, N):
-    x = Linear(type, M, K, N, seed=M + K + N)
+def test_shapes(ws, type, M, K, N, pad, shift):
+    x = Linear(type, M, K, N, pad=pad, shift=shift, seed=M + K + N)
     x.call(ws)
     x.check()
 
 
 @BOTH
+@PLACES
 @pytest.mark.parametrize("M,K,N", SHAPES)
-def test_gated_shapes(ws, type, M, K, N):
-    x = Linear(type, M, K, N, act="silu", gated=True, seed=M + K + N + 1)
+def test_gated_shapes(ws, type, M, K, N, pad, shift):
+    x = Linear(type, M, K, N, act="silu", gated=True, pad=pad, shift=shift, seed=M + K + N + 1)
     x.call(ws)
     x.check()
 
@@ -84,9 +90,10 @@ def test_bias_or_residual(ws, type, bias, residual, M, K, N):
 @pytest.mark.parametrize("M,K,N", [(1, 16384, 64), (4, 8192, 100), (64, 8192, 48), (64, 16000, 260), (130, 8200, 70),
                                    (200, 9000, 256), (300, 4096, 500)])
 @pytest.mark.parametrize("gated", [False, True])
-def test_long_sums(ws, type, M, K, N, gated):
+@pytest.mark.parametrize("pad", [8, 32, "lines"])
+def test_long_sums(ws, type, M, K, N, gated, pad):
     """Few tiles and a long K: slices of K over several workgroups."""
-    x = Linear(type, M, K, N, act="silu" if gated else "none", gated=gated, residual=True, seed=K)
+    x = Linear(type, M, K, N, act="silu" if gated else "none", gated=gated, residual=True, pad=pad, seed=K)
     x.call(ws)
     x.check()
     first = x.y.clone()
@@ -178,11 +185,17 @@ def test_activations_of_infinities(ws):
 
 
 @BOTH
-def test_strides(ws, type):
-    """Rows far apart, as slices of one wide buffer; the widest stride there is."""
-    x = Linear(type, 70, 40, 72, pad=4096, residual=True)
+@pytest.mark.parametrize("M", [3, 20, 70, 200])
+@pytest.mark.parametrize("pad", [0, 8, 16, 24, 32, 40, 48, 56, 4096])
+def test_strides(ws, type, M, pad):
+    """Every place of a row in a line; rows far apart, as slices of one wide buffer."""
+    x = Linear(type, M, 200, 72, pad=pad, residual=True)
     x.call(ws)
     x.check()
+
+
+@BOTH
+def test_widest_stride(ws, type):
     far = Linear(type, 2, 16, 9, pad=(1 << 22) - 16)
     assert far.x.stride(0) == 1 << 22
     far.call(ws)
