@@ -202,6 +202,29 @@ def test_widest_stride(ws, type):
     far.check()
 
 
+@pytest.mark.parametrize("gated", [False, True])
+@pytest.mark.parametrize("M,K,N", [(1, 70, 90), (40, 136, 90), (129, 200, 260), (2337, 65, 2682)])
+def test_widest_strides_of_every_tile(ws, gated, M, K, N):
+    """Rows and weights at the widest stride: a tile's offsets end just below 2^31."""
+    wide = 1 << 22
+    far = Linear("bf16", M, K, N, act="silu" if gated else "none", gated=gated, seed=M)
+    for name in ("x", "w", "w_up") if gated else ("x", "w"):
+        t = getattr(far, name)
+        buf = torch.empty((t.shape[0], wide), dtype=t.dtype, device="cuda")
+        buf[:, :K + 8] = math.nan
+        buf[:, :K].copy_(t)
+        setattr(far, name, buf[:, :K])
+    far.call(ws)
+    far.check()
+
+
+@pytest.mark.parametrize("M,N", [(1, 20), (20, 9)])
+def test_longest_rows(ws, M, N):
+    x = Linear("f16", M, (1 << 22) - 3, N, pad=0, seed=N)
+    x.call(ws)
+    x.check()
+
+
 def test_weights_beyond_2_gib(ws):
     x = Linear("bf16", 5, 8192, 8)
     N = 140000

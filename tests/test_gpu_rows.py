@@ -90,6 +90,20 @@ def test_norm_in_place(type, M, N, out, into):
     x.check(ref)
 
 
+@BOTH
+@pytest.mark.parametrize("h,y", [("x", "partial"), ("partial", "x"), ("peer", "partial")])
+@pytest.mark.parametrize("M,N", [(3, 40), (67, 900), (1100, 2050), (9, 16384)])
+def test_norm_with_both_outputs_in_place(type, M, N, h, y):
+    x = Norm(type, M, N, 2, seed=5)
+    ref = x.reference()
+    th, ty = getattr(x, h), getattr(x, y)
+    x.call(h=p(th), ld_h=ld(th), y=p(ty), ld_y=ld(ty))
+    torch.cuda.synchronize()
+    x.h.copy_(th)
+    x.y.copy_(ty)
+    x.check(ref)
+
+
 @pytest.mark.parametrize("N", [8, 500, 5000])
 @pytest.mark.parametrize("size,eps", [(3e38, 1e-5), (1e25, 0.0), (1e-30, 0.0), (1e-20, 1e-5), (1e-38, 0.0), (1e-22, 1e-42)])
 def test_norm_of_any_bf16_numbers(N, size, eps):
