@@ -663,8 +663,8 @@ vt_status vt_paged_chunk_attn(const vt_paged_kv* kv, const vt_paged_io* io, floa
  * are never written. Infinities and NaN in a row or a weight reach the results as in the formulas. Everything
  * but the descriptors is device memory of the current device, and ``stream`` is one of that device. Up to 2^20
  * rows a call. The projections are fastest where rows start at 128-byte lines (x, w and w_up at such addresses, their ld
- * multiples of 64): other rows cost up to a fifth of a product of many rows and up to a third where reading 64 rows' weights
- * is all of the time, nothing up to 16 rows. */
+ * multiples of 64). Other row strides cost little up to a thousand rows and up to a third of a product of more rows; matrices that do
+ * not even start at a line cost a third where reading the weights of a batch is all of the time. */
 
 /* Activation functions: z, max(z, 0), z / (1 + exp(-z)), z Phi(z) with the normal distribution's
  * Phi, and its approximation z (1 + tanh(sqrt(2 / pi) (z + 0.044715 z^3))) / 2. VT_ACT_RELU of NaN is 0. */

@@ -207,7 +207,8 @@ class LdsOnce {
 };
 
 hipError_t launch_thin(const Args& a, bool bf16, bool gated, hipStream_t s);
-hipError_t launch_mid(const Args& a, int which, bool bf16, bool gated, hipStream_t s);  // of kMid
+// ``which``: of kMid. ``shift``: whole lines of rows that do not start at them (of matrices that do).
+hipError_t launch_mid(const Args& a, int which, bool shift, bool bf16, bool gated, hipStream_t s);
 hipError_t launch_tile(const Args& a, bool bf16, bool gated, hipStream_t s);
 
 }  // namespace lin

@@ -15,20 +15,28 @@
 // Rows past the matrices' ends are read from their last row (the sums are never stored). The stage that reaches
 // past K goes through registers, masked, and is multiplied first.
 //
+// Where rows do not start at 128-byte lines, 128 bytes of a row are in two lines, and each line is asked for twice, half of it
+// a time, which memory serves at half its rate. SHIFT loads whole lines: a stage holds a line of each row, from the one of
+// the row's start on, whose last chunks are the row's next ones. They lie where a row's chunks always do, so reads meet no
+// bank conflict, and a lane takes its chunk from a stage or from the next one. Since 8 rows are whole lines, which of them depends on
+// the row within the fragment alone: a lane's place in LDS is its own, and goes round the ring. It
+// keeps one more stage; the stage past K comes last and its fragments are masked.
+// The matrices themselves have to start at lines, else there would be reads before them. (Measured, bf16: 64 rows of 4104 numbers
+// through 14336 features 39 -> 28 us, as at 4096; 777 rows of 3302 through 4096 42 -> 37; with the weights in
+// memory 640 rows of 3920 through 11678 118 -> 84; what the choice costs elsewhere is in linear.hip. With chunks where
+// they lie in their lines, conflicts in LDS cost half of that again.)
+//
 // What bounds it: up to about 64 rows reading the weights, above it LDS (at 128 x 128 its reads and the loads' writes take
 // 768 cycles of a stage, the products 512). Measured in bf16: 64 rows of 8192 through the gate and up projections of
 // 7168 features 48 to 55 us, 4.3 to 4.9 TB/s; rows of 4096 through 4096 features: 256 rows 18 us (474 TFLOP/s),
-// 512 25 (676), 1024 40 (853); 777 rows of 3302 to 4096 with a residual 39 to 43, 30 at 3328. Rows that do not start at
-// 128-byte lines cost that: half of each line is fetched again for the next stage. Tried for them and not kept, since
-// each lost more elsewhere: whole lines into LDS and fragments from two stages (64 rows through 14336 features 32
-// us, not 39, but 20 to 60% slower wherever the weights were in the caches), and two stages' loads together (777 rows 38,
-// not 42, other sizes 2 to 15% slower). 64 x 64 per wave on the large tile's schedule: 0 to 8% faster than 128 x 128 here.
+// 512 25 (676), 1024 40 (853). Tried at 128 x 128 and not kept: 64 x 64 per wave on the large tile's schedule, 8% faster to
+// 19% slower; two stages' loads together, 3% slower on average.
 #include "linear_lds.hpp"
 
 namespace vt {
 namespace lin {
 
-template <class T, bool GATED, int WR, int WC, int MBW, int NBW, int ST>
+template <class T, bool GATED, int WR, int WC, int MBW, int NBW, int ST, bool SHIFT>
 __global__ void __launch_bounds__(WR* WC* kWave) mid_kernel(Args a) {
   constexpr int NW = WR * WC, XB = WR * MBW, WB = WC * NBW;  // waves; 16-row blocks of rows and of weights
   constexpr int U = 2 * (XB + WB), LPS = U / NW;              // units (8 rows x 64 k) of a stage, loads of a wave
@@ -47,51 +55,64 @@ __global__ void __launch_bounds__(WR* WC* kWave) mid_kernel(Args a) {
 
   // This wave loads units wave, wave + NW, .. of a stage: unit v is half v % 2 of block v / 2, the rows' first.
   const int rows_x = min(TM, a.M - m0), rows_w = min(TN, a.N - n0);
-  const u32x4 rx = rsrc_words(a.x + m0 * a.ld_x, static_cast<uint32_t>(rows_x * a.ld_x * 2));
-  const u32x4 rw0 = rsrc_words(a.w[0] + n0 * a.ld_w[0], static_cast<uint32_t>(rows_w * a.ld_w[0] * 2));
-  const u32x4 rw1 = GATED ? rsrc_words(a.w[1] + n0 * a.ld_w[1], static_cast<uint32_t>(rows_w * a.ld_w[1] * 2)) : rw0;
+  // up to the last 8 numbers of the last row: a line that SHIFT loads may go on past them
+  auto matrix = [&](const uint16_t* p, int64_t ld, int first, int rows) {
+    return rsrc_words(p + first * ld, static_cast<uint32_t>(((rows - 1) * ld + (a.K + 7) / 8 * 8) * 2));
+  };
+  const u32x4 rx = matrix(a.x, a.ld_x, m0, rows_x), rw0 = matrix(a.w[0], a.ld_w[0], n0, rows_w);
+  const u32x4 rw1 = GATED ? matrix(a.w[1], a.ld_w[1], n0, rows_w) : rw0;
+  // chunks (8 numbers) by which a row starts into its line
+  auto into_line = [](int64_t row, int64_t ld) { return SHIFT ? static_cast<int>(row * ld / 8) % 8 : 0; };
   u32x4 rs[LPS];
   uint32_t off[LPS];
 #pragma unroll
   for (int i = 0; i < LPS; ++i) {
     const int v = wave + NW * i, b = v / 2, half = v % 2, brow = 8 * half + block_row(lane);
+    int64_t ld = a.ld_x;
+    int row;
+    rs[i] = rx;
     if (b < XB) {
-      rs[i] = rx;
-      off[i] = static_cast<uint32_t>(min(16 * b + brow, rows_x - 1) * a.ld_x * 2);
+      row = min(16 * b + brow, rows_x - 1);
     } else {
       const int wb = b - XB, fb = wb % NBW, fo = fb % NBO;
       const bool up = GATED && fb >= NBO;
       const int in = PW == 8 ? 32 * (fo / 2) + 8 * (brow / 4) + 4 * (fo % 2) + brow % 4 : 16 * fo + brow;
-      const int row = min(wb / NBW * NBO * 16 + in, rows_w - 1);
+      row = min(wb / NBW * NBO * 16 + in, rows_w - 1);
+      ld = up ? a.ld_w[1] : a.ld_w[0];
       rs[i] = up ? rw1 : rw0;
-      off[i] = static_cast<uint32_t>(row * (up ? a.ld_w[1] : a.ld_w[0]) * 2);
     }
-    off[i] += block_chunk(lane, half) * 16;
+    const int skip = into_line(row, ld);
+    off[i] = static_cast<uint32_t>(row * ld * 2) - skip * 16 + (block_chunk(lane, half) + skip) % 8 * 16;
   }
   const uint32_t place0 = lds_address(lds) + wave * 1024;
-  int next = kt0, left = kt1 - kt0;
+  int next = kt0, left = SHIFT ? KT + 1 : kt1 - kt0;
+  if (SHIFT) {  // lines may go on past the matrix: the offsets whose range is checked are the lanes' whole ones
+#pragma unroll
+    for (int i = 0; i < LPS; ++i) off[i] += static_cast<uint32_t>(kt0) * (TK * 2);
+  }
   // Past the last stage the loads go on with empty ranges from offset 0 (no memory traffic, stages that nobody
   // reads), so the counts stay.
   auto load = [&](uint32_t stage) {
     const bool more = left > 0;
-    const uint32_t at = more ? static_cast<uint32_t>(next) * (TK * 2) : 0u;
+    const uint32_t at = more && !SHIFT ? static_cast<uint32_t>(next) * (TK * 2) : 0u;
     each<LPS>([&](auto I) {
       constexpr int i = decltype(I)::value;
       u32x4 r = rs[i];
       r.z = more ? r.z : 0u;
       put_fetch<i * NW * 1024>(place0 + stage, r, off[i], at);
+      if (SHIFT) off[i] += TK * 2;
     });
     ++next;
     --left;
   };
 
-  const int wr = wave / WC, wc = wave % WC, fa = lane % 16 / 8 * 1024 + fragment_at(lane);
+  const int wr = wave / WC, wc = wave % WC;
   f32x4 acc[NBW][MBW];
 #pragma unroll
   for (int f = 0; f < NBW; ++f)
 #pragma unroll
     for (int b = 0; b < MBW; ++b) acc[f][b] = f32x4{0.f, 0.f, 0.f, 0.f};
-  if (tail) {  // to stage 0, with zeros past K
+  if (tail && !SHIFT) {  // to stage 0, with zeros past K
 #pragma unroll
     for (int i = 0; i < LPS; ++i) {
       const int u = wave + NW * i, k = full * TK + block_chunk(lane, u % 2) * 8;
@@ -101,31 +122,70 @@ __global__ void __launch_bounds__(WR* WC* kWave) mid_kernel(Args a) {
   }
   each<ST - 1>([&](auto Q) {
     constexpr int q = decltype(Q)::value;
-    if (q > 0 || !tail) load(q * STAGE);
+    if (q > 0 || !tail || SHIFT) load(q * STAGE);
   });
+  // Where this lane's parts of the fragments are (in the block of their first row, with SHIFT in the ring): of rows, and of the
+  // gate's and the up projection's even and odd blocks, for both k-steps.
+  uint32_t fx[2], fw[GATED ? 2 : 1][2][2];
+  auto spot = [&](int row, int64_t ld, int h) {
+    const int chunk = 4 * h + lane / 16;
+    return static_cast<uint32_t>((lane % 16 / 8 * 1024 + (fragment_at(lane) ^ (h * 64))) + (chunk + into_line(row, ld)) / 8 * STAGE);
+  };
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int r = lane % 16;
+    fx[h] = spot(r, a.ld_x, h);
+#pragma unroll
+    for (int m = 0; m < (GATED ? 2 : 1); ++m)
+#pragma unroll
+      for (int odd = 0; odd < 2; ++odd) fw[m][odd][h] = spot(PW == 8 ? 4 * odd + r % 4 : r, a.ld_w[m], h);
+  }
   uint32_t cur = 0, into = (ST - 1) * STAGE;
-  for (int q = 0; q < KT; ++q) {
-    // all but the newest ST - 2 stages' loads of this wave, and its reads of the stage before
-    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(LPS * (ST - 2)) : "memory");
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
-    load(into);
+  auto up = [](uint32_t x) { return x + STAGE == ST * STAGE ? 0u : x + STAGE; };
+  auto turn = [](uint32_t& x) { x = min(x + STAGE, x + STAGE - ST * STAGE); };  // (below 0 is large)
+  auto multiply = [&](auto MASK) {
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const char* S = lds + cur + (fa ^ (h * 64));
+      auto read = [&](uint32_t at, int block) {
+        const u32x4 v = *reinterpret_cast<const u32x4*>(lds + (SHIFT ? 0u : cur) + at + block * 2048);
+        if constexpr (decltype(MASK)::value) return keep_first(v, a.K - (full * TK + h * 32 + lane / 16 * 8));
+        return v;
+      };
       u32x4 xf[MBW], wf[NBW];
 #pragma unroll
-      for (int b = 0; b < MBW; ++b) xf[b] = *reinterpret_cast<const u32x4*>(S + (wr * MBW + b) * 2048);
+      for (int b = 0; b < MBW; ++b) xf[b] = read(fx[h], wr * MBW + b);
 #pragma unroll
-      for (int f = 0; f < NBW; ++f) wf[f] = *reinterpret_cast<const u32x4*>(S + (XB + wc * NBW + f) * 2048);
+      for (int f = 0; f < NBW; ++f) wf[f] = read(fw[f / NBO][f % NBO % 2][h], XB + wc * NBW + f);
 #pragma unroll
       for (int f = 0; f < NBW; ++f)
 #pragma unroll
         for (int b = 0; b < MBW; ++b) acc[f][b] = T::mfma16(wf[f], xf[b], acc[f][b]);
     }
+    if (SHIFT) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        turn(fx[h]);
+#pragma unroll
+        for (int m = 0; m < (GATED ? 2 : 1); ++m) {
+          turn(fw[m][0][h]);
+          if (NBO > 1) turn(fw[m][1][h]);
+        }
+      }
+    }
+  };
+  auto step = [&](auto MASK) {
+    // all but the newest stages' loads of this wave (with SHIFT the next one is there too), and its reads of the stage before
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(LPS * (SHIFT ? ST - 3 : ST - 2)) : "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    load(into);
+    multiply(MASK);
     into = cur;
-    cur = cur + STAGE == ST * STAGE ? 0 : cur + STAGE;
-  }
+    cur = up(cur);
+  };
+  const int plain = SHIFT && tail ? KT - 1 : KT;
+  for (int q = 0; q < plain; ++q) step(std::false_type{});
+  if (SHIFT && tail) step(std::true_type{});
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // no load is on its way into LDS when a wave ends
 
   if (a.splits > 1 && !join<NBW, MBW, NW>(a, acc, lds, m_tile * a.n_tiles + n_tile, split, wave, lane)) return;
@@ -156,28 +216,32 @@ struct Kernel {
   int threads, lds;
 };
 
-template <int WR, int WC, int MBW, int NBW, int ST>
+template <int WR, int WC, int MBW, int NBW, int ST, bool SHIFT>
 constexpr Kernel kernel() {
-  return {{mid_kernel<Half, false, WR, WC, MBW, NBW, ST>, mid_kernel<Half, true, WR, WC, MBW, NBW, ST>,
-           mid_kernel<BFloat, false, WR, WC, MBW, NBW, ST>, mid_kernel<BFloat, true, WR, WC, MBW, NBW, ST>},
+  return {{mid_kernel<Half, false, WR, WC, MBW, NBW, ST, SHIFT>, mid_kernel<Half, true, WR, WC, MBW, NBW, ST, SHIFT>,
+           mid_kernel<BFloat, false, WR, WC, MBW, NBW, ST, SHIFT>, mid_kernel<BFloat, true, WR, WC, MBW, NBW, ST, SHIFT>},
           WR * WC * kWave,
           ST * 2 * (WR * MBW + WC * NBW) * 1024};
 }
 
-// in the order of kMid
-const Kernel kKernels[] = {kernel<1, 2, 1, 2, 5>(), kernel<2, 2, 1, 2, 4>(), kernel<4, 2, 1, 2, 4>(),
-                           kernel<4, 2, 1, 4, 4>(), kernel<4, 2, 2, 4, 4>()};
+// in the order of kMid, rows at lines and not
+const Kernel kKernels[][2] = {{kernel<1, 2, 1, 2, 5, false>(), kernel<1, 2, 1, 2, 6, true>()},
+                              {kernel<2, 2, 1, 2, 4, false>(), kernel<2, 2, 1, 2, 5, true>()},
+                              {kernel<4, 2, 1, 2, 4, false>(), kernel<4, 2, 1, 2, 5, true>()},
+                              {kernel<4, 2, 1, 4, 4, false>(), kernel<4, 2, 1, 4, 5, true>()},
+                              {kernel<4, 2, 2, 4, 4, false>(), kernel<4, 2, 2, 4, 5, true>()}};
 
 }  // namespace
 
-hipError_t launch_mid(const Args& a, int which, bool bf16, bool gated, hipStream_t s) {
+hipError_t launch_mid(const Args& a, int which, bool shift, bool bf16, bool gated, hipStream_t s) {
   static LdsOnce once;
   const hipError_t e = once([](auto&& raise) {
-    for (const Kernel& k : kKernels)
-      for (auto* f : k.run) raise(reinterpret_cast<const void*>(f), k.lds);
+    for (const auto& pair : kKernels)
+      for (const Kernel& k : pair)
+        for (auto* f : k.run) raise(reinterpret_cast<const void*>(f), k.lds);
   });
   if (e != hipSuccess) return e;
-  const Kernel& k = kKernels[which];
+  const Kernel& k = kKernels[which][shift];
   hipLaunchKernelGGL(k.run[2 * bf16 + gated], dim3(static_cast<uint32_t>(grid_of(a.m_tiles, a.n_tiles * a.splits))),
                      dim3(k.threads), k.lds, s, a);
   return hipGetLastError();

@@ -184,6 +184,23 @@ def test_activations_of_infinities(ws):
         assert bool(got[3:].isfinite().all())
 
 
+# large weights, whose rows are loaded by lines, for each tile between single rows and prompts, whole and in slices of K
+COLD = [(1, 1389, 12276), (1, 1538, 11308), (1, 618, 13746), (5, 1476, 5766), (11, 10155, 1669), (1, 6659, 2570), (3, 4632, 1831),
+        (1, 11844, 731), (18, 1259, 13486), (31, 1283, 13507), (30, 1151, 7369), (9, 1223, 7833), (17, 9562, 1774), (17, 3523, 4835),
+        (29, 8895, 953), (17, 13381, 646), (64, 4715, 16356), (41, 3960, 8319), (34, 4038, 4170), (77, 2951, 9826),
+        (81, 3013, 4764), (200, 520, 16652)]
+
+
+@BOTH
+@pytest.mark.parametrize("pad", [0, 8, 24, 48])
+@pytest.mark.parametrize("gated", [False, True])
+@pytest.mark.parametrize("M,K,N", COLD)
+def test_rows_of_large_weights_between_lines(ws, type, M, K, N, gated, pad):
+    x = Linear(type, M, K, N, act="silu" if gated else "none", gated=gated, pad=pad, seed=M + K)
+    x.call(ws)
+    x.check()
+
+
 @BOTH
 @pytest.mark.parametrize("M", [3, 20, 70, 200])
 @pytest.mark.parametrize("pad", [0, 8, 16, 24, 32, 40, 48, 56, 4096])
