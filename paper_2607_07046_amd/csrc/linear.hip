@@ -41,21 +41,21 @@ vt_status check_shape(const vt_linear_io* io) {
 //   + (slices > 1) (join + part * slices' MB + slice * slices):
 // rounds of 256 workgroups (one per compute unit; those that fit beside each other overlap in ``step``), steps of 64 k of a
 // slice, MB read and written once, MB that the tiles load. The constants are fitted to 4000 products of random sizes (1 to 8192
-// rows, 64 to 16384 in, 16 to 32768 out, both kinds, every kernel and slice count): median error 4 to 8%, the
-// choice 1.8% slower than the best of all measured on average, 7% in one of ten, 23% in one of a hundred.
-// Without the kernel named the products are slower by (mean, worst): thin 1.3%, 1.2 times; 32 rows 0.8%, 1.3; 64 rows
-// 0.8%, 1.1; 64 x 128 0.5%, 1.25; 256 x 128 0.5%, 1.5; 256 x 256 0.7%, 1.5; 128 x 128 0.3%, 1.2; 16 x 64 0.2%, 1.1.
+// rows, 64 to 16384 in, 16 to 32768 out, both kinds, every kernel and slice count): median error 5 to 7%, the
+// choice 1.7% slower than the best of all measured on average, 6% in one of ten, 21% in one of a hundred.
+// Without the kernel named the products are slower by (mean, worst): thin 1.2%, 1.4 times; 16 x 64 0.6%, 1.2; 32 rows 2.1%,
+// 1.5; 64 x 64 2.4%, 1.4; 64 x 128 0.5%, 1.2; 128 x 128 1.6%, 1.5; 256 x 128 0.4%, 1.3; 256 x 256 0.7%, 1.4.
 struct Cost {
   double start, step, tile, memory, l2, join, part, slice;
 };
-constexpr Cost kThinCost = {3.407, 0.0566, 0.156, 0.1243, 0.0, 1.275, 1.487, 0.097};
-constexpr Cost kMidCost[] = {{3.439, 0.1371, 0.151, 0.0975, 0.0, 1.111, 0.427, 0.066},
-                             {3.073, 0.1447, 0.360, 0.0973, 0.0, 1.220, 0.322, 0.097},
-                             {2.863, 0.1901, 0.825, 0.0530, 0.00912, 1.480, 0.266, 0.136},
-                             {1.706, 0.2589, 2.297, 0.0731, 0.01407, 2.096, 0.260, 0.240},
-                             {1.794, 0.4144, 3.204, 0.0268, 0.02384, 2.011, 0.182, 0.583}};
-constexpr Cost kNarrowCost = {3.620, 0.5503, 5.360, 0.0649, 0.02155, 0, 0, 0};
-constexpr Cost kWideCost = {5.131, 0.9108, 9.962, 0.0434, 0.02568, 0, 0, 0};
+constexpr Cost kThinCost = {3.229, 0.0581, 0.218, 0.1129, 0.0, 1.308, 1.572, 0.088};
+constexpr Cost kMidCost[] = {{3.127, 0.1331, 0.196, 0.0924, 0.0, 1.186, 0.593, 0.071},
+                             {2.991, 0.1480, 0.306, 0.0930, 0.0, 1.266, 0.379, 0.102},
+                             {2.897, 0.1247, 1.035, 0.0644, 0.0180, 1.561, 0.288, 0.140},
+                             {1.593, 0.1747, 2.809, 0.0832, 0.0166, 2.299, 0.244, 0.244},
+                             {1.815, 0.2781, 3.941, 0.0336, 0.0244, 2.304, 0.167, 0.588}};
+constexpr Cost kNarrowCost = {3.664, 0.5164, 5.510, 0.0616, 0.0234, 0, 0, 0};
+constexpr Cost kWideCost = {5.332, 0.8521, 9.889, 0.0549, 0.0271, 0, 0, 0};
 constexpr int kSlices[] = {1, 2, 3, 4, 6, 8, 12, 16};
 constexpr int kThinRows = 16;  // beyond, the thin tile reads the weights more than once
 constexpr int kUnits = 256;    // compute units

@@ -1,10 +1,15 @@
 // Products of a batch's or a short prompt's rows: vt_linear and vt_linear_gated on tiles between those of
 // linear_thin.hip and linear_tile.hip.
 //
-// WR x WC waves of 16 MBW rows x 16 NBW weight rows each. Both operands come straight into LDS through a
+// WR x WC places of 16 MBW rows x 16 NBW weight rows each. Both operands come straight into LDS through a
 // ring of ST stages of 64 k, up to ST - 1 of them on the way, each number once per tile; the
-// waves wait for a stage by the count of their own loads and meet once per stage. Two workgroups
-// share a compute unit, so one multiplies while the other waits.
+// waves wait for a stage by the count of their own loads and meet once per stage.
+//
+// On tiles of 64 rows and more two waves share a place and take one of a stage's two k-steps each (KW = 2): a place can
+// then be twice as high, and LDS, which bounds these tiles, is read two thirds as much (128 x 128: 64 KiB of a stage, not 96). The
+// next stage's fragments are read, and loads sent out, between single products. The two waves' sums meet in LDS at the end, half
+// of the rows for each. A stage takes 0.125 us at 64 x 64, 0.175 at 64 x 128 and 0.278 at 128 x 128, where one wave per
+// place that read, then multiplied took 0.190, 0.259 and 0.414.
 //
 // The product's first operand is the weights: a lane's accumulators are consecutive features of a row. The weight
 // rows of two blocks are dealt to them four by four in turn, so a lane has 8 consecutive features,
@@ -22,27 +27,28 @@
 // the row within the fragment alone: a lane's place in LDS is its own, and goes round the ring. It
 // keeps one more stage; the stage past K comes last and its fragments are masked.
 // The matrices themselves have to start at lines, else there would be reads before them. (Measured, bf16: 64 rows of 4104 numbers
-// through 14336 features 39 -> 28 us, as at 4096; 777 rows of 3302 through 4096 42 -> 37; with the weights in
-// memory 640 rows of 3920 through 11678 118 -> 84; what the choice costs elsewhere is in linear.hip. With chunks where
+// through 14336 features 39 -> 28 us, as at 4096; with the weights in memory 640 rows of 3920 through 11678 118 -> 84; what the choice costs elsewhere is in linear.hip. With chunks where
 // they lie in their lines, conflicts in LDS cost half of that again.)
 //
-// What bounds it: up to about 64 rows reading the weights, above it LDS (at 128 x 128 its reads and the loads' writes take
-// 768 cycles of a stage, the products 512). Measured in bf16: 64 rows of 8192 through the gate and up projections of
-// 7168 features 48 to 55 us, 4.3 to 4.9 TB/s; rows of 4096 through 4096 features: 256 rows 18 us (474 TFLOP/s),
-// 512 25 (676), 1024 40 (853). Tried at 128 x 128 and not kept: 64 x 64 per wave on the large tile's schedule, 8% faster to
-// 19% slower; two stages' loads together, 3% slower on average.
+// What bounds it: up to about 64 rows reading the weights, above it LDS (at 128 x 128 the products of a stage take 512 cycles, the
+// fragments' reads 512 and the loads' writes 256; it takes about 650). Measured in bf16: 64 rows of 8192 through the gate and
+// up projections of 7168 features 48 to 55 us, 4.3 to 4.9 TB/s; rows of 4096 through 4096 features: 256 rows 16 us
+// (530 TFLOP/s), 512 23 (760), 1024 34 (1010); 777 rows of 3302 through 4096 with a residual 32. Tried at 128 x 128 and not
+// kept: a quarter of the products ahead of the meeting point, no faster; the large tile's schedule for four waves; three stages of 64 x 128,
+// so that two workgroups fit, 1% slower.
 #include "linear_lds.hpp"
 
 namespace vt {
 namespace lin {
 
-template <class T, bool GATED, int WR, int WC, int MBW, int NBW, int ST, bool SHIFT>
-__global__ void __launch_bounds__(WR* WC* kWave) mid_kernel(Args a) {
-  constexpr int NW = WR * WC, XB = WR * MBW, WB = WC * NBW;  // waves; 16-row blocks of rows and of weights
+template <class T, bool GATED, int WR, int WC, int KW, int MBW, int NBW, int ST, bool SHIFT>
+__global__ void __launch_bounds__(WR* WC* KW* kWave) mid_kernel(Args a) {
+  constexpr int NW = WR * WC * KW, XB = WR * MBW, WB = WC * NBW;  // waves; 16-row blocks of rows and of weights
   constexpr int U = 2 * (XB + WB), LPS = U / NW;              // units (8 rows x 64 k) of a stage, loads of a wave
   constexpr int NBO = GATED ? NBW / 2 : NBW;                 // 16-feature blocks of a wave
   constexpr int TM = 16 * XB, TN = 16 * WC * NBO, TK = 64, STAGE = U * 1024, PW = NBO % 2 ? 4 : 8;
-  static_assert(U % NW == 0 && (!GATED || NBW % 2 == 0), "");
+  constexpr int HS = 2 / KW, MBO = MBW / KW;                  // k-steps of a stage, row blocks of the result, of a wave
+  static_assert(U % NW == 0 && (!GATED || NBW % 2 == 0) && KW <= 2 && MBW % KW == 0, "");
   extern __shared__ __attribute__((aligned(16))) char lds[];
   int m_tile, unit;
   if (!my_tile(blockIdx.x, a.m_tiles, a.n_tiles * a.splits, TM, m_tile, unit)) return;
@@ -90,23 +96,26 @@ __global__ void __launch_bounds__(WR* WC* kWave) mid_kernel(Args a) {
 #pragma unroll
     for (int i = 0; i < LPS; ++i) off[i] += static_cast<uint32_t>(kt0) * (TK * 2);
   }
-  // Past the last stage the loads go on with empty ranges from offset 0 (no memory traffic, stages that nobody
-  // reads), so the counts stay.
-  auto load = [&](uint32_t stage) {
+  // Past the last stage the loads go on with empty ranges (no memory traffic, stages that nobody multiplies), so the
+  // counts stay.
+  auto load1 = [&](auto I, uint32_t stage) {
+    constexpr int i = decltype(I)::value;
     const bool more = left > 0;
-    const uint32_t at = more && !SHIFT ? static_cast<uint32_t>(next) * (TK * 2) : 0u;
-    each<LPS>([&](auto I) {
-      constexpr int i = decltype(I)::value;
-      u32x4 r = rs[i];
-      r.z = more ? r.z : 0u;
-      put_fetch<i * NW * 1024>(place0 + stage, r, off[i], at);
-      if (SHIFT) off[i] += TK * 2;
-    });
+    u32x4 r = rs[i];
+    r.z = more ? r.z : 0u;
+    put_fetch<i * NW * 1024>(place0 + stage, r, off[i], more && !SHIFT ? static_cast<uint32_t>(next) * (TK * 2) : 0u);
+    if (SHIFT) off[i] += TK * 2;
+  };
+  auto advance = [&]() {
     ++next;
     --left;
   };
+  auto load = [&](uint32_t stage) {
+    each<LPS>([&](auto I) { load1(I, stage); });
+    advance();
+  };
 
-  const int wr = wave / WC, wc = wave % WC;
+  const int kw = wave / (WR * WC), wr = wave / WC % WR, wc = wave % WC;
   f32x4 acc[NBW][MBW];
 #pragma unroll
   for (int f = 0; f < NBW; ++f)
@@ -120,19 +129,19 @@ __global__ void __launch_bounds__(WR* WC* kWave) mid_kernel(Args a) {
       *reinterpret_cast<u32x4*>(lds + u * 1024 + lane * 16) = keep_first(v, a.K - k);
     }
   }
-  each<ST - 1>([&](auto Q) {
+  each<(KW == 2 ? ST : ST - 1)>([&](auto Q) {
     constexpr int q = decltype(Q)::value;
     if (q > 0 || !tail || SHIFT) load(q * STAGE);
   });
   // Where this lane's parts of the fragments are (in the block of their first row, with SHIFT in the ring): of rows, and of the
   // gate's and the up projection's even and odd blocks, for both k-steps.
-  uint32_t fx[2], fw[GATED ? 2 : 1][2][2];
+  uint32_t fx[HS], fw[GATED ? 2 : 1][2][HS];
   auto spot = [&](int row, int64_t ld, int h) {
-    const int chunk = 4 * h + lane / 16;
-    return static_cast<uint32_t>((lane % 16 / 8 * 1024 + (fragment_at(lane) ^ (h * 64))) + (chunk + into_line(row, ld)) / 8 * STAGE);
+    const int ks = kw * HS + h, chunk = 4 * ks + lane / 16;
+    return static_cast<uint32_t>(lane % 16 / 8 * 1024 + (fragment_at(lane) ^ (ks * 64)) + (chunk + into_line(row, ld)) / 8 * STAGE);
   };
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
+  for (int h = 0; h < HS; ++h) {
     const int r = lane % 16;
     fx[h] = spot(r, a.ld_x, h);
 #pragma unroll
@@ -140,59 +149,150 @@ __global__ void __launch_bounds__(WR* WC* kWave) mid_kernel(Args a) {
 #pragma unroll
       for (int odd = 0; odd < 2; ++odd) fw[m][odd][h] = spot(PW == 8 ? 4 * odd + r % 4 : r, a.ld_w[m], h);
   }
-  uint32_t cur = 0, into = (ST - 1) * STAGE;
+  uint32_t cur = 0;
   auto up = [](uint32_t x) { return x + STAGE == ST * STAGE ? 0u : x + STAGE; };
   auto turn = [](uint32_t& x) { x = min(x + STAGE, x + STAGE - ST * STAGE); };  // (below 0 is large)
-  auto multiply = [&](auto MASK) {
+  u32x4 xf[2][MBW], wf[2][NBW];
+  // fragment i of k-step h of the stage at ``from``
+  auto read1 = [&](int i, int set, int h, uint32_t from) {
+    const char* at = lds + (SHIFT ? 0u : from);
+    if (i < MBW) {
+      xf[set][i] = *reinterpret_cast<const u32x4*>(at + fx[h] + (wr * MBW + i) * 2048);
+    } else {
+      const int f = i - MBW;
+      wf[set][f] = *reinterpret_cast<const u32x4*>(at + fw[f / NBO][f % NBO % 2][h] + (XB + wc * NBW + f) * 2048);
+    }
+  };
+  auto turn_all = [&](int h) {
+    if (!SHIFT) return;
+    turn(fx[h]);
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      auto read = [&](uint32_t at, int block) {
-        const u32x4 v = *reinterpret_cast<const u32x4*>(lds + (SHIFT ? 0u : cur) + at + block * 2048);
-        if constexpr (decltype(MASK)::value) return keep_first(v, a.K - (full * TK + h * 32 + lane / 16 * 8));
-        return v;
-      };
-      u32x4 xf[MBW], wf[NBW];
+    for (int m = 0; m < (GATED ? 2 : 1); ++m) {
+      turn(fw[m][0][h]);
+      if (NBO > 1) turn(fw[m][1][h]);
+    }
+  };
+  auto read = [&](auto SET, int h, uint32_t from) {
 #pragma unroll
-      for (int b = 0; b < MBW; ++b) xf[b] = read(fx[h], wr * MBW + b);
+    for (int i = 0; i < MBW + NBW; ++i) read1(i, decltype(SET)::value, h, from);
+    turn_all(h);
+  };
+  auto mask = [&](auto SET, int h) {
+    constexpr int set = decltype(SET)::value;
+    const int keep = a.K - (full * TK + (kw * HS + h) * 32 + lane / 16 * 8);
 #pragma unroll
-      for (int f = 0; f < NBW; ++f) wf[f] = read(fw[f / NBO][f % NBO % 2][h], XB + wc * NBW + f);
+    for (int b = 0; b < MBW; ++b) xf[set][b] = keep_first(xf[set][b], keep);
+#pragma unroll
+    for (int f = 0; f < NBW; ++f) wf[set][f] = keep_first(wf[set][f], keep);
+  };
+  auto multiply = [&](auto SET) {
+    constexpr int set = decltype(SET)::value;
+#pragma unroll
+    for (int f = 0; f < NBW; ++f)
+#pragma unroll
+      for (int b = 0; b < MBW; ++b) acc[f][b] = T::mfma16(wf[set][f], xf[set][b], acc[f][b]);
+  };
+  auto meet = [&](auto N) {  // all but the newest N stages' loads of this wave have arrived, and its fragments
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(LPS * decltype(N)::value) : "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+  };
+  using S0 = std::integral_constant<int, 0>;
+  using S1 = std::integral_constant<int, 1>;
+  const int plain = SHIFT && tail ? KT - 1 : KT;
+  if constexpr (KW == 2) {
+    constexpr int P = MBW * NBW;
+    static_assert(MBW + NBW <= P && 2 * LPS <= P, "room beside the products");
+    // A stage is one k-step of this wave. The next one's fragments are read beside its products, so its own are in registers when
+    // the waves meet, and the stage is free for the loads.
+    meet(std::integral_constant<int, SHIFT ? ST - 2 : ST - 1>{});
+    read(S0{}, 0, 0);
+    auto step = [&](auto SET) {
+      meet(std::integral_constant<int, SHIFT ? ST - 3 : ST - 2>{});
+      const uint32_t next_stage = up(cur);
+      each<P>([&](auto I) {  // a product, and what goes out beside it
+        constexpr int i = decltype(I)::value, set = decltype(SET)::value, f = i / MBW, b = i % MBW;
+        acc[f][b] = T::mfma16(wf[set][f], xf[set][b], acc[f][b]);
+        if constexpr (i == 0) __builtin_amdgcn_sched_barrier(0);  // (else it is made to wait for the first read)
+        if constexpr (i < MBW + NBW) read1(i, 1 - set, 0, next_stage);
+        if constexpr (i % 2 == 1 && i / 2 < LPS) load1(std::integral_constant<int, i / 2>{}, cur);
+        __builtin_amdgcn_sched_barrier(0);
+      });
+      turn_all(0);
+      advance();
+      cur = next_stage;
+    };
+    int q = 0;
+    for (; q + 1 < plain; q += 2) {
+      step(S0{});
+      step(S1{});
+    }
+    if (q < plain) step(S0{});
+    if (SHIFT && tail) {
+      if (q < plain) {
+        mask(S1{}, 0);
+        multiply(S1{});
+      } else {
+        mask(S0{}, 0);
+        multiply(S0{});
+      }
+    }
+  } else {
+    uint32_t into = (ST - 1) * STAGE;
+    auto step = [&](auto MASK) {
+      meet(std::integral_constant<int, SHIFT ? ST - 3 : ST - 2>{});
+      load(into);
+      read(S0{}, 0, cur);
+      read(S1{}, HS - 1, cur);
+      if constexpr (decltype(MASK)::value) {
+        mask(S0{}, 0);
+        mask(S1{}, HS - 1);
+      }
+      multiply(S0{});
+      multiply(S1{});
+      into = cur;
+      cur = up(cur);
+    };
+    for (int q = 0; q < plain; ++q) step(std::false_type{});
+    if (SHIFT && tail) step(std::true_type{});
+  }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // no load is on its way into LDS when a wave ends
+
+  // The result's blocks of this wave: with KW waves on a tile's place each takes a share of the rows, from all.
+  f32x4 out[NBW][MBO];
+  if constexpr (KW == 2) {
+    __syncthreads();  // the ring is free
+    auto give = [&](int b0) {
 #pragma unroll
       for (int f = 0; f < NBW; ++f)
 #pragma unroll
-        for (int b = 0; b < MBW; ++b) acc[f][b] = T::mfma16(wf[f], xf[b], acc[f][b]);
-    }
-    if (SHIFT) {
+        for (int b = 0; b < MBO; ++b)
+          *reinterpret_cast<f32x4*>(lds + (wave * NBW * MBO + f * MBO + b) * 1024 + lane * 16) = acc[f][b0 + b];
+    };
+    if (kw == 0) give(MBO);
+    else give(0);
+    __syncthreads();
+    const int other = kw ? wave - WR * WC : wave + WR * WC;
+    auto take = [&](int b0) {
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        turn(fx[h]);
+      for (int f = 0; f < NBW; ++f)
 #pragma unroll
-        for (int m = 0; m < (GATED ? 2 : 1); ++m) {
-          turn(fw[m][0][h]);
-          if (NBO > 1) turn(fw[m][1][h]);
-        }
-      }
-    }
-  };
-  auto step = [&](auto MASK) {
-    // all but the newest stages' loads of this wave (with SHIFT the next one is there too), and its reads of the stage before
-    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(LPS * (SHIFT ? ST - 3 : ST - 2)) : "memory");
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
-    load(into);
-    multiply(MASK);
-    into = cur;
-    cur = up(cur);
-  };
-  const int plain = SHIFT && tail ? KT - 1 : KT;
-  for (int q = 0; q < plain; ++q) step(std::false_type{});
-  if (SHIFT && tail) step(std::true_type{});
-  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // no load is on its way into LDS when a wave ends
-
-  if (a.splits > 1 && !join<NBW, MBW, NW>(a, acc, lds, m_tile * a.n_tiles + n_tile, split, wave, lane)) return;
+        for (int b = 0; b < MBO; ++b)
+          out[f][b] = acc[f][b0 + b] + *reinterpret_cast<f32x4*>(lds + (other * NBW * MBO + f * MBO + b) * 1024 + lane * 16);
+    };
+    if (kw == 0) take(0);
+    else take(MBO);
+  } else {
+#pragma unroll
+    for (int f = 0; f < NBW; ++f)
+#pragma unroll
+      for (int b = 0; b < MBO; ++b) out[f][b] = acc[f][b];
+  }
+  if (a.splits > 1 && !join<NBW, MBO, NW>(a, out, lds, m_tile * a.n_tiles + n_tile, split, wave, lane)) return;
 
 #pragma unroll
-  for (int b = 0; b < MBW; ++b) {
-    const int m = m0 + (wr * MBW + b) * 16 + lane % 16;
+  for (int b = 0; b < MBO; ++b) {
+    const int m = m0 + (wr * MBW + kw * MBO + b) * 16 + lane % 16;
     if (m >= a.M) continue;
 #pragma unroll
     for (int f = 0; f < NBO; f += PW / 4) {
@@ -201,8 +301,8 @@ __global__ void __launch_bounds__(WR* WC* kWave) mid_kernel(Args a) {
       float z[PW], u[PW];
 #pragma unroll
       for (int e = 0; e < PW; ++e) {
-        z[e] = acc[f + e / 4][b][e % 4];
-        u[e] = GATED ? acc[NBO + f + e / 4][b][e % 4] : 0.f;
+        z[e] = out[f + e / 4][b][e % 4];
+        u[e] = GATED ? out[NBO + f + e / 4][b][e % 4] : 0.f;
       }
       finish<T, GATED, PW>(a, m, n, z, u);
     }
@@ -216,20 +316,20 @@ struct Kernel {
   int threads, lds;
 };
 
-template <int WR, int WC, int MBW, int NBW, int ST, bool SHIFT>
+template <int WR, int WC, int KW, int MBW, int NBW, int ST, bool SHIFT>
 constexpr Kernel kernel() {
-  return {{mid_kernel<Half, false, WR, WC, MBW, NBW, ST, SHIFT>, mid_kernel<Half, true, WR, WC, MBW, NBW, ST, SHIFT>,
-           mid_kernel<BFloat, false, WR, WC, MBW, NBW, ST, SHIFT>, mid_kernel<BFloat, true, WR, WC, MBW, NBW, ST, SHIFT>},
-          WR * WC * kWave,
+  return {{mid_kernel<Half, false, WR, WC, KW, MBW, NBW, ST, SHIFT>, mid_kernel<Half, true, WR, WC, KW, MBW, NBW, ST, SHIFT>,
+           mid_kernel<BFloat, false, WR, WC, KW, MBW, NBW, ST, SHIFT>, mid_kernel<BFloat, true, WR, WC, KW, MBW, NBW, ST, SHIFT>},
+          WR * WC * KW * kWave,
           ST * 2 * (WR * MBW + WC * NBW) * 1024};
 }
 
 // in the order of kMid, rows at lines and not
-const Kernel kKernels[][2] = {{kernel<1, 2, 1, 2, 5, false>(), kernel<1, 2, 1, 2, 6, true>()},
-                              {kernel<2, 2, 1, 2, 4, false>(), kernel<2, 2, 1, 2, 5, true>()},
-                              {kernel<4, 2, 1, 2, 4, false>(), kernel<4, 2, 1, 2, 5, true>()},
-                              {kernel<4, 2, 1, 4, 4, false>(), kernel<4, 2, 1, 4, 5, true>()},
-                              {kernel<4, 2, 2, 4, 4, false>(), kernel<4, 2, 2, 4, 5, true>()}};
+const Kernel kKernels[][2] = {{kernel<1, 2, 1, 1, 2, 5, false>(), kernel<1, 2, 1, 1, 2, 6, true>()},
+                              {kernel<2, 2, 1, 1, 2, 4, false>(), kernel<2, 2, 1, 1, 2, 5, true>()},
+                              {kernel<2, 2, 2, 2, 2, 4, false>(), kernel<2, 2, 2, 2, 2, 5, true>()},
+                              {kernel<2, 2, 2, 2, 4, 4, false>(), kernel<2, 2, 2, 2, 4, 5, true>()},
+                              {kernel<2, 2, 2, 4, 4, 4, false>(), kernel<2, 2, 2, 4, 4, 5, true>()}};
 
 }  // namespace
 

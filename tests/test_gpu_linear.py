@@ -32,7 +32,25 @@ LARGE = [(20, 898, 75), (2279, 1322, 9), (754, 1846, 30), (1089, 2307, 21), (288
          (2337, 65, 2682), (3785, 33, 4161), (4115, 200, 3319), (3380, 1, 3699), (3869, 359, 3362), (2500, 448, 4008),
          (862, 256, 5974), (1249, 1, 4901), (1420, 1, 8586), (2774, 64, 4459), (3939, 75, 5250), (3887, 1, 3044),
          (2046, 64, 5268)]
-SHAPES += LARGE
+# and for those of 64 rows and more: one stage of K, an even and an odd number, an end inside the last
+TILES = [(1, 3551, 8980), (1, 4295, 8222), (2, 4928, 8693), (2, 4992, 8339), (17, 7546, 8599), (17, 8289, 4387),
+         (17, 8606, 8925), (21, 7859, 4111), (21, 8196, 4315), (33, 129, 8422), (33, 200, 8639), (34, 193, 4397),
+         (34, 6339, 4540), (35, 130, 5545), (53, 120, 4275), (53, 128, 4164), (66, 139, 6083), (66, 3776, 5273),
+         (66, 4274, 4180), (66, 4516, 8705), (66, 5763, 6497), (66, 6627, 2942), (67, 6208, 2145), (67, 6528, 2165),
+         (69, 7488, 5157), (70, 6714, 5486), (71, 4672, 4116), (75, 3713, 4254), (97, 1, 6690), (121, 135, 8276),
+         (129, 64, 4940), (161, 67, 7615), (162, 137, 5661), (166, 75, 7414), (204, 1, 7025), (225, 137, 4116),
+         (228, 128, 5252), (293, 64, 4934), (294, 65, 5003), (325, 128, 7642), (357, 65, 7069), (446, 192, 2365),
+         (514, 140, 3955), (585, 6592, 579), (772, 72, 2031), (817, 128, 7266), (1047, 8, 1483), (1100, 128, 1369),
+         (1130, 192, 1795), (1141, 8, 6521), (1349, 129, 705), (1384, 7123, 1), (1434, 6912, 1), (1470, 8, 2511),
+         (1797, 128, 6884), (1826, 8, 7693), (2026, 1, 8250), (2059, 4800, 1), (2145, 4480, 1), (2385, 8, 7507),
+         (2446, 130, 845), (2617, 64, 1164), (2728, 2503, 1), (2749, 3264, 1), (2764, 2754, 1), (2825, 2721, 1),
+         (2870, 2652, 1), (3086, 1, 2307), (3089, 3617, 1), (3214, 8, 454), (3284, 64, 1093), (3427, 64, 4623),
+         (3431, 3015, 1), (3503, 1, 7306), (3841, 1, 3436), (3858, 1, 5510), (3887, 8, 7086), (3905, 21, 5517),
+         (3957, 64, 5276), (4120, 150, 36), (4162, 1, 707), (4163, 72, 593), (4226, 5824, 66), (4236, 64, 1666),
+         (4317, 2375, 1), (4325, 8512, 66), (4340, 192, 217), (4344, 8, 173), (4467, 6021, 74), (4476, 8321, 66),
+         (4484, 2178, 1), (4489, 8643, 41), (4610, 2368, 6), (4689, 2368, 2), (4770, 1, 749), (4777, 2304, 1),
+         (4847, 5379, 77), (4901, 8, 622), (4920, 1, 282), (4952, 2242, 4), (4978, 142, 69), (4981, 64, 260)]
+SHAPES += LARGE + TILES
 
 
 # rows between 128-byte lines, at them, and matrices that start between them
