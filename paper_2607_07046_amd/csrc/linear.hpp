@@ -116,17 +116,37 @@ __device__ __forceinline__ float one(const uint16_t* p) {
   return a;
 }
 
+// The first numbers of a group of W (4 or 8), fewer than W and as many in every lane: in pieces of 4, 2 and 1, whose places
+// are the same for all lanes.
+template <int W, class V>
+__device__ __forceinline__ void store_first(uint16_t* y, V v, int count) {
+  int at = 0;
+  uint32_t lo = v[0], hi = v[1];
+  if (W == 8 && (count & 4)) {
+    *reinterpret_cast<pg::u32x2*>(y) = pg::u32x2{lo, hi};
+    at = 4;
+    lo = v[W / 2 - 2];
+    hi = v[W / 2 - 1];
+  }
+  if (count & 2) {
+    *reinterpret_cast<uint32_t*>(y + at) = lo;
+    at += 2;
+    lo = hi;
+  }
+  if (count & 1) y[at] = static_cast<uint16_t>(lo);
+}
+
 // W (4 or 8) consecutive features n.. of row m, from the product's sums to y. Whole groups by wide
-// accesses; the group that reaches past N by single numbers, so no byte outside is read or written
-// but a row's own. (Both paths end in the same vector:
+// accesses; of the group that reaches past N the bias is read by single numbers, the residual as it is (rows may be read up to a
+// multiple of 8) and nothing past N is written. (Both paths end in the same vector:
 // stores to z and u on either side of the branch were merged into one at a variable index, in scratch memory.)
 template <class T, bool GATED, int W>
 __device__ __forceinline__ void finish(const Args& a, int m, int n, float (&z)[W], float (&u)[W]) {
   typedef unsigned int vec __attribute__((ext_vector_type(W / 2)));
   const bool whole = n + W <= a.N;
-  auto add = [&](const uint16_t* p, float (&to)[W]) {
+  auto add = [&](const uint16_t* p, bool all, float (&to)[W]) {
     vec v;
-    if (whole) {
+    if (all) {
       v = *reinterpret_cast<const vec*>(p);
     } else {
       each<W / 2>([&](auto E) {
@@ -142,14 +162,14 @@ __device__ __forceinline__ void finish(const Args& a, int m, int n, float (&z)[W
       to[2 * e + 1] += hi;
     });
   };
-  if (a.bias[0]) add(a.bias[0] + n, z);
+  if (a.bias[0]) add(a.bias[0] + n, whole, z);
   activate(z, a.act);
   if (GATED) {
-    if (a.bias[1]) add(a.bias[1] + n, u);
+    if (a.bias[1]) add(a.bias[1] + n, whole, u);
 #pragma unroll
     for (int e = 0; e < W; ++e) z[e] *= u[e];
   }
-  if (a.res) add(a.res + m * a.ld_r + n, z);
+  if (a.res) add(a.res + m * a.ld_r + n, true, z);
   uint16_t* y = a.y + m * a.ld_y + n;
   vec v;
   each<W / 2>([&](auto E) {
@@ -159,10 +179,7 @@ __device__ __forceinline__ void finish(const Args& a, int m, int n, float (&z)[W
   if (whole) {
     *reinterpret_cast<vec*>(y) = v;
   } else {
-    each<W>([&](auto E) {
-      constexpr int e = decltype(E)::value;
-      if (n + e < a.N) y[e] = static_cast<uint16_t>(v[e / 2] >> (16 * (e % 2)));
-    });
+    store_first<W>(y, v, a.N % W);
   }
 }
 

@@ -223,7 +223,7 @@ __device__ __forceinline__ void tile(const Args& a, char* lds, int m_tile, int n
     lds_sync();
     u32x4 cur_r[PB], nxt_r[PB];
     auto ahead = [&](int r0, u32x4 (&to)[PB]) {
-      if (!a.res || !whole) return;
+      if (!a.res || !there) return;
 #pragma unroll
       for (int p = 0; p < PB; ++p) {
         const int m = min(ms + r0 + p * RPP + lane / LPR, a.M - 1);
@@ -256,26 +256,20 @@ __device__ __forceinline__ void tile(const Args& a, char* lds, int m_tile, int n
             for (int e = 0; e < 8; ++e) z[e] *= u[e];
           }
           uint16_t* y = a.y + m * a.ld_y + n;
-          if (whole) {
-            if (a.res) {
+          if (a.res) {
 #pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                float lo, hi;
-                T::unpack2(cur_r[p][e], lo, hi);
-                z[2 * e] += lo;
-                z[2 * e + 1] += hi;
-              }
+            for (int e = 0; e < 4; ++e) {
+              float lo, hi;
+              T::unpack2(cur_r[p][e], lo, hi);
+              z[2 * e] += lo;
+              z[2 * e + 1] += hi;
             }
-            u32x4 v;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] = T::pack2(z[2 * e], z[2 * e + 1]);
-            *reinterpret_cast<u32x4*>(y) = v;
-          } else {
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-              if (n + e < a.N)
-                y[e] = static_cast<uint16_t>(T::pack2(z[e] + (a.res ? one<T>(a.res + m * a.ld_r + n + e) : 0.f), 0.f));
           }
+          u32x4 v;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[e] = T::pack2(z[2 * e], z[2 * e + 1]);
+          if (whole) *reinterpret_cast<u32x4*>(y) = v;
+          else store_first<8>(y, v, a.N % 8);
         }
       }
 #pragma unroll

@@ -4,6 +4,7 @@
 #include <cmath>
 
 #include "internal.hpp"
+#include "linear.hpp"
 #include "paged_append.hpp"
 
 namespace vt {
@@ -54,9 +55,11 @@ __device__ __forceinline__ S row_sum(S v, S* red) {
 // h = x + partial + peer, y = h / sqrt(mean(h^2) + eps) * gain. TR threads take a row and hold it in registers,
 // V groups of 8 numbers each, so every number is read and written once: memory bounds it. Measured: 8192 rows of 5120 with a
 // partial sum, bf16, 67 to 69 us, 4.9 to 5.0 TB/s; 64 rows of 8192 with a partial and the peers' sum 4.3 us in a captured graph.
+constexpr int threads(int tr) { return tr <= 128 ? 256 : tr; }
+
 template <class T, int TR, int V>
-__global__ void __launch_bounds__(TR < 256 ? 256 : TR) norm_kernel(NormArgs a) {
-  constexpr int NT = TR < 256 ? 256 : TR, RPB = NT / TR;
+__global__ void __launch_bounds__(threads(TR)) norm_kernel(NormArgs a) {
+  constexpr int NT = threads(TR), RPB = NT / TR;
   __shared__ double red[NT / kWave];
   const int t = threadIdx.x % TR;
   const int row = blockIdx.x * RPB + threadIdx.x / TR;
@@ -70,7 +73,14 @@ __global__ void __launch_bounds__(TR < 256 ? 256 : TR) norm_kernel(NormArgs a) {
     wx[i] = load16(a.x + r * a.ld_x + c);
     if (a.partial) wp[i] = load16(a.partial + r * a.ld_partial + c);
     if (a.peer) wq[i] = load16(a.peer + r * a.ld_peer + c);
-    if (c + 8 <= a.N) wg[i] = load16(a.gain + c);
+    if (c + 8 <= a.N) {
+      wg[i] = load16(a.gain + c);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        wg[i][e] = (c + 2 * e < a.N ? a.gain[c + 2 * e] : 0u) |
+                   (c + 2 * e + 1 < a.N ? static_cast<uint32_t>(a.gain[c + 2 * e + 1]) << 16 : 0u);
+    }
   }
   float h[V][8];
   float ss = 0.f;
@@ -103,13 +113,8 @@ __global__ void __launch_bounds__(TR < 256 ? 256 : TR) norm_kernel(NormArgs a) {
     }
     if (a.h && there) {
       uint16_t* p = a.h + r * a.ld_h + c;
-      if (whole) {
-        *reinterpret_cast<u32x4*>(p) = w;
-      } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-          if (c + e < a.N) p[e] = static_cast<uint16_t>(w[e / 2] >> (16 * (e % 2)));
-      }
+      if (whole) *reinterpret_cast<u32x4*>(p) = w;
+      else lin::store_first<8>(p, w, a.N % 8);
     }
 #pragma unroll
     for (int e = 0; e < 8; ++e) ss = fmaf(h[i][e], h[i][e], ss);
@@ -136,29 +141,14 @@ __global__ void __launch_bounds__(TR < 256 ? 256 : TR) norm_kernel(NormArgs a) {
     const int c = (i * TR + t) * 8;
     if (c >= a.N) continue;
     float g[8];
-    const bool whole = c + 8 <= a.N;
-    if (whole) {
-      unpack<T>(wg[i], g);
-    } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        float hi;
-        g[e] = 0.f;
-        if (c + e < a.N) T::unpack2(a.gain[c + e], g[e], hi);
-      }
-    }
+    unpack<T>(wg[i], g);
     float y[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) y[e] = out ? static_cast<float>(h[i][e] * wide * g[e]) : h[i][e] * inv * g[e];
     const u32x4 w = packed<T>(y);
     uint16_t* p = a.y + r * a.ld_y + c;
-    if (whole) {
-      *reinterpret_cast<u32x4*>(p) = w;
-    } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e)
-        if (c + e < a.N) p[e] = static_cast<uint16_t>(w[e / 2] >> (16 * (e % 2)));
-    }
+    if (c + 8 <= a.N) *reinterpret_cast<u32x4*>(p) = w;
+    else lin::store_first<8>(p, w, a.N % 8);
   }
 }
 
@@ -171,19 +161,20 @@ namespace {
 
 constexpr int kMaxRows = 1 << 20, kMaxHidden = 16384;
 
+// The fewest threads, in whole waves, that hold a row: idle ones cost (8192 rows of 2049 numbers on 512 threads 39 us, on 320 35; of 5120
+// on 1024 71, on 640 69).
+template <class T, int V, int TR, int... MORE>
+void launch_norm(const rows::NormArgs& a, hipStream_t s) {
+  if constexpr (sizeof...(MORE) > 0)
+    if (a.N > TR * V * 8) return launch_norm<T, V, MORE...>(a, s);
+  constexpr int NT = rows::threads(TR), RPB = NT / TR;
+  hipLaunchKernelGGL((rows::norm_kernel<T, TR, V>), dim3((a.M + RPB - 1) / RPB), dim3(NT), 0, s, a);
+}
+
 template <class T>
 void launch_norm(const rows::NormArgs& a, hipStream_t s) {
-  const int chunks = (a.N + 7) / 8;
-  auto go = [&](auto* k, int tr) {
-    const int nt = tr < 256 ? 256 : tr, rpb = nt / tr;
-    hipLaunchKernelGGL(k, dim3((a.M + rpb - 1) / rpb), dim3(nt), 0, s, a);
-  };
-  if (chunks <= 64) return go(rows::norm_kernel<T, 64, 1>, 64);
-  if (chunks <= 128) return go(rows::norm_kernel<T, 128, 1>, 128);
-  if (chunks <= 256) return go(rows::norm_kernel<T, 256, 1>, 256);
-  if (chunks <= 512) return go(rows::norm_kernel<T, 512, 1>, 512);
-  if (chunks <= 1024) return go(rows::norm_kernel<T, 1024, 1>, 1024);
-  return go(rows::norm_kernel<T, 1024, 2>, 1024);
+  if (a.N <= 8192) return launch_norm<T, 1, 64, 128, 192, 256, 320, 384, 448, 512, 640, 768, 896, 1024>(a, s);
+  launch_norm<T, 2, 640, 768, 896, 1024>(a, s);
 }
 
 }  // namespace
