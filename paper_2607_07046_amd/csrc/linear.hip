@@ -42,20 +42,20 @@ vt_status check_shape(const vt_linear_io* io) {
 // rounds of 256 workgroups (one per compute unit; those that fit beside each other overlap in ``step``), steps of 64 k of a
 // slice, MB read and written once, MB that the tiles load. The constants are fitted to 4000 products of random sizes (1 to 8192
 // rows, 64 to 16384 in, 16 to 32768 out, both kinds, every kernel and slice count): median error 5 to 7%, the
-// choice 1.7% slower than the best of all measured on average, 6% in one of ten, 21% in one of a hundred.
-// Without the kernel named the products are slower by (mean, worst): thin 1.2%, 1.4 times; 16 x 64 0.6%, 1.2; 32 rows 2.1%,
-// 1.5; 64 x 64 2.4%, 1.4; 64 x 128 0.5%, 1.2; 128 x 128 1.6%, 1.5; 256 x 128 0.4%, 1.3; 256 x 256 0.7%, 1.4.
+// choice 1.9% slower than the best of all measured on average, 8% in one of ten, 22% in one of a hundred.
+// Without the kernel named the products are slower by (mean, worst): thin 0.9%, 1.3 times; 16 x 64 0.9%, 1.2; 32 rows 2.8%,
+// 1.4; 64 x 64 2.4%, 1.4; 64 x 128 0.5%, 1.2; 128 x 128 1.5%, 1.5; 256 x 128 0.6%, 1.3; 256 x 256 0.9%, 1.4.
 struct Cost {
   double start, step, tile, memory, l2, join, part, slice;
 };
-constexpr Cost kThinCost = {3.229, 0.0581, 0.218, 0.1129, 0.0, 1.308, 1.572, 0.088};
-constexpr Cost kMidCost[] = {{3.127, 0.1331, 0.196, 0.0924, 0.0, 1.186, 0.593, 0.071},
-                             {2.991, 0.1480, 0.306, 0.0930, 0.0, 1.266, 0.379, 0.102},
-                             {2.897, 0.1247, 1.035, 0.0644, 0.0180, 1.561, 0.288, 0.140},
-                             {1.593, 0.1747, 2.809, 0.0832, 0.0166, 2.299, 0.244, 0.244},
-                             {1.815, 0.2781, 3.941, 0.0336, 0.0244, 2.304, 0.167, 0.588}};
-constexpr Cost kNarrowCost = {3.664, 0.5164, 5.510, 0.0616, 0.0234, 0, 0, 0};
-constexpr Cost kWideCost = {5.332, 0.8521, 9.889, 0.0549, 0.0271, 0, 0, 0};
+constexpr Cost kThinCost = {3.247, 0.0582, 0.202, 0.1123, 0.0, 1.217, 1.557, 0.094};
+constexpr Cost kMidCost[] = {{3.087, 0.1322, 0.194, 0.0922, 0.0, 1.122, 0.578, 0.073},
+                             {2.991, 0.0981, 0.464, 0.1073, 0.0110, 1.217, 0.381, 0.094},
+                             {2.905, 0.1241, 0.999, 0.0640, 0.0182, 1.472, 0.279, 0.139},
+                             {1.609, 0.1736, 2.757, 0.0826, 0.0171, 2.223, 0.234, 0.242},
+                             {1.827, 0.2763, 3.842, 0.0316, 0.0261, 2.242, 0.163, 0.572}};
+constexpr Cost kNarrowCost = {2.544, 0.5143, 5.432, 0.0584, 0.0253, 0, 0, 0};
+constexpr Cost kWideCost = {3.319, 0.8613, 9.745, 0.0473, 0.0299, 0, 0, 0};
 constexpr int kSlices[] = {1, 2, 3, 4, 6, 8, 12, 16};
 constexpr int kThinRows = 16;  // beyond, the thin tile reads the weights more than once
 constexpr int kUnits = 256;    // compute units

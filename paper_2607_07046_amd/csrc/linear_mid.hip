@@ -5,11 +5,11 @@
 // ring of ST stages of 64 k, up to ST - 1 of them on the way, each number once per tile; the
 // waves wait for a stage by the count of their own loads and meet once per stage.
 //
-// On tiles of 64 rows and more two waves share a place and take one of a stage's two k-steps each (KW = 2): a place can
+// On tiles of 32 rows and more two waves share a place and take one of a stage's two k-steps each (KW = 2): a place can
 // then be twice as high, and LDS, which bounds these tiles, is read two thirds as much (128 x 128: 64 KiB of a stage, not 96). The
 // next stage's fragments are read, and loads sent out, between single products. The two waves' sums meet in LDS at the end, half
-// of the rows for each. A stage takes 0.125 us at 64 x 64, 0.175 at 64 x 128 and 0.278 at 128 x 128, where one wave per
-// place that read, then multiplied took 0.190, 0.259 and 0.414.
+// of the rows for each. A stage takes 0.098 us at 32 x 64, 0.125 at 64 x 64, 0.175 at 64 x 128 and 0.278 at 128 x 128, where one wave per
+// place that read, then multiplied took 0.148, 0.190, 0.259 and 0.414.
 //
 // The product's first operand is the weights: a lane's accumulators are consecutive features of a row. The weight
 // rows of two blocks are dealt to them four by four in turn, so a lane has 8 consecutive features,
@@ -91,7 +91,7 @@ __global__ void __launch_bounds__(WR* WC* KW* kWave) mid_kernel(Args a) {
     off[i] = static_cast<uint32_t>(row * ld * 2) - skip * 16 + (block_chunk(lane, half) + skip) % 8 * 16;
   }
   const uint32_t place0 = lds_address(lds) + wave * 1024;
-  int next = kt0, left = SHIFT ? KT + 1 : kt1 - kt0;
+  int next = kt0 + (SHIFT || kt1 <= kt0 ? 0 : first_of(blockIdx.x, kt1 - kt0)), left = SHIFT ? KT + 1 : kt1 - kt0;
   if (SHIFT) {  // lines may go on past the matrix: the offsets whose range is checked are the lanes' whole ones
 #pragma unroll
     for (int i = 0; i < LPS; ++i) off[i] += static_cast<uint32_t>(kt0) * (TK * 2);
@@ -107,7 +107,7 @@ __global__ void __launch_bounds__(WR* WC* KW* kWave) mid_kernel(Args a) {
     if (SHIFT) off[i] += TK * 2;
   };
   auto advance = [&]() {
-    ++next;
+    if (++next == kt1 && !SHIFT) next = kt0;
     --left;
   };
   auto load = [&](uint32_t stage) {
@@ -202,7 +202,8 @@ __global__ void __launch_bounds__(WR* WC* KW* kWave) mid_kernel(Args a) {
   const int plain = SHIFT && tail ? KT - 1 : KT;
   if constexpr (KW == 2) {
     constexpr int P = MBW * NBW;
-    static_assert(MBW + NBW <= P && 2 * LPS <= P, "room beside the products");
+    static_assert(MBW + NBW <= P && LPS <= P, "room beside the products");
+    constexpr bool ROOM = 2 * LPS <= P;
     // A stage is one k-step of this wave. The next one's fragments are read beside its products, so its own are in registers when
     // the waves meet, and the stage is free for the loads.
     meet(std::integral_constant<int, SHIFT ? ST - 2 : ST - 1>{});
@@ -215,7 +216,8 @@ __global__ void __launch_bounds__(WR* WC* KW* kWave) mid_kernel(Args a) {
         acc[f][b] = T::mfma16(wf[set][f], xf[set][b], acc[f][b]);
         if constexpr (i == 0) __builtin_amdgcn_sched_barrier(0);  // (else it is made to wait for the first read)
         if constexpr (i < MBW + NBW) read1(i, 1 - set, 0, next_stage);
-        if constexpr (i % 2 == 1 && i / 2 < LPS) load1(std::integral_constant<int, i / 2>{}, cur);
+        if constexpr (ROOM ? i % 2 == 1 && i / 2 < LPS : i >= P - LPS)
+          load1(std::integral_constant<int, ROOM ? i / 2 : i - (P - LPS)>{}, cur);
         __builtin_amdgcn_sched_barrier(0);
       });
       turn_all(0);
@@ -326,7 +328,7 @@ constexpr Kernel kernel() {
 
 // in the order of kMid, rows at lines and not
 const Kernel kKernels[][2] = {{kernel<1, 2, 1, 1, 2, 5, false>(), kernel<1, 2, 1, 1, 2, 6, true>()},
-                              {kernel<2, 2, 1, 1, 2, 4, false>(), kernel<2, 2, 1, 1, 2, 5, true>()},
+                              {kernel<1, 2, 2, 2, 2, 4, false>(), kernel<1, 2, 2, 2, 2, 5, true>()},
                               {kernel<2, 2, 2, 2, 2, 4, false>(), kernel<2, 2, 2, 2, 2, 5, true>()},
                               {kernel<2, 2, 2, 2, 4, 4, false>(), kernel<2, 2, 2, 2, 4, 5, true>()},
                               {kernel<2, 2, 2, 4, 4, 4, false>(), kernel<2, 2, 2, 4, 4, 5, true>()}};

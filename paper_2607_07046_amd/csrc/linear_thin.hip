@@ -47,11 +47,11 @@ __global__ void __launch_bounds__(NW* kWave) thin_kernel(Args a) {
   for (int f = 0; f < FB; ++f) acc[f] = f32x4{0.f, 0.f, 0.f, 0.f};
   u32x4 wf[DEPTH][FB][HS], xf[DEPTH][HS];
   const int full = a.K / KS, s0 = split * a.steps;
-  const int s1 = min(s0 + a.steps, full);
+  const int s1 = min(s0 + a.steps, full), count = max(s1 - s0, 0), first = count ? first_of(blockIdx.x, count) : 0;
   // step i of this wave; past the slice's end nothing is read and zeros are multiplied
   auto load = [&](int i, u32x4 (&w)[FB][HS], u32x4 (&x)[HS]) {
-    const int s = s0 + wave + i * NW;
-    const uint32_t gone = s < s1 ? 0u : kOOB, at = s < s1 ? static_cast<uint32_t>(s * KS * 2) : 0u;
+    const int j = wave + i * NW, s = j + first < count ? j + first : j + first - count;
+    const uint32_t gone = j < count ? 0u : kOOB, at = j < count ? static_cast<uint32_t>((s0 + s) * KS * 2) : 0u;
 #pragma unroll
     for (int h = 0; h < HS; ++h) {
 #pragma unroll

@@ -66,7 +66,7 @@ __device__ __forceinline__ void tile(const Args& a, char* lds, int m_tile, int n
   }
   // A half's loads of this wave, the rows' first. Past the last k-tile they go on with empty
   // ranges from offset 0 (no memory traffic, slots that nobody reads), so the counts stay.
-  uint32_t koff = 0;
+  uint32_t koff = full ? first_of(blockIdx.x, full) * (TK * 2) : 0;
   int left = full;
   const uint32_t placex = lbase + wave * LX * 1024, placew = lbase + XB + wave * (NB / 2) * 1024;
   auto place = [&](int i) { return i < LX ? placex : placew; };
@@ -86,6 +86,7 @@ __device__ __forceinline__ void tile(const Args& a, char* lds, int m_tile, int n
   };
   auto advance = [&]() {  // after both halves of a k-tile
     koff += TK * 2;
+    if (koff == static_cast<uint32_t>(full) * (TK * 2)) koff = 0;
     if (--left <= 0) none_left();
   };
   auto stage_tail = [&]() {  // the k-tile that reaches past K, with zeros there, to the first two slots

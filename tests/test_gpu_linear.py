@@ -32,24 +32,30 @@ LARGE = [(20, 898, 75), (2279, 1322, 9), (754, 1846, 30), (1089, 2307, 21), (288
          (2337, 65, 2682), (3785, 33, 4161), (4115, 200, 3319), (3380, 1, 3699), (3869, 359, 3362), (2500, 448, 4008),
          (862, 256, 5974), (1249, 1, 4901), (1420, 1, 8586), (2774, 64, 4459), (3939, 75, 5250), (3887, 1, 3044),
          (2046, 64, 5268)]
-# and for those of 64 rows and more: one stage of K, an even and an odd number, an end inside the last
-TILES = [(1, 3551, 8980), (1, 4295, 8222), (2, 4928, 8693), (2, 4992, 8339), (17, 7546, 8599), (17, 8289, 4387),
-         (17, 8606, 8925), (21, 7859, 4111), (21, 8196, 4315), (33, 129, 8422), (33, 200, 8639), (34, 193, 4397),
-         (34, 6339, 4540), (35, 130, 5545), (53, 120, 4275), (53, 128, 4164), (66, 139, 6083), (66, 3776, 5273),
-         (66, 4274, 4180), (66, 4516, 8705), (66, 5763, 6497), (66, 6627, 2942), (67, 6208, 2145), (67, 6528, 2165),
-         (69, 7488, 5157), (70, 6714, 5486), (71, 4672, 4116), (75, 3713, 4254), (97, 1, 6690), (121, 135, 8276),
-         (129, 64, 4940), (161, 67, 7615), (162, 137, 5661), (166, 75, 7414), (204, 1, 7025), (225, 137, 4116),
-         (228, 128, 5252), (293, 64, 4934), (294, 65, 5003), (325, 128, 7642), (357, 65, 7069), (446, 192, 2365),
-         (514, 140, 3955), (585, 6592, 579), (772, 72, 2031), (817, 128, 7266), (1047, 8, 1483), (1100, 128, 1369),
-         (1130, 192, 1795), (1141, 8, 6521), (1349, 129, 705), (1384, 7123, 1), (1434, 6912, 1), (1470, 8, 2511),
-         (1797, 128, 6884), (1826, 8, 7693), (2026, 1, 8250), (2059, 4800, 1), (2145, 4480, 1), (2385, 8, 7507),
-         (2446, 130, 845), (2617, 64, 1164), (2728, 2503, 1), (2749, 3264, 1), (2764, 2754, 1), (2825, 2721, 1),
-         (2870, 2652, 1), (3086, 1, 2307), (3089, 3617, 1), (3214, 8, 454), (3284, 64, 1093), (3427, 64, 4623),
-         (3431, 3015, 1), (3503, 1, 7306), (3841, 1, 3436), (3858, 1, 5510), (3887, 8, 7086), (3905, 21, 5517),
-         (3957, 64, 5276), (4120, 150, 36), (4162, 1, 707), (4163, 72, 593), (4226, 5824, 66), (4236, 64, 1666),
-         (4317, 2375, 1), (4325, 8512, 66), (4340, 192, 217), (4344, 8, 173), (4467, 6021, 74), (4476, 8321, 66),
-         (4484, 2178, 1), (4489, 8643, 41), (4610, 2368, 6), (4689, 2368, 2), (4770, 1, 749), (4777, 2304, 1),
-         (4847, 5379, 77), (4901, 8, 622), (4920, 1, 282), (4952, 2242, 4), (4978, 142, 69), (4981, 64, 260)]
+# and for those of 32 rows and more: one stage of K, an even and an odd number, an end inside the last
+TILES = [(1, 3551, 8980), (2, 4928, 8693), (17, 377, 1), (17, 384, 1), (17, 426, 1), (17, 832, 1), (17, 7168, 5161),
+         (17, 7546, 8599), (17, 8606, 8925), (18, 326, 1), (18, 345, 1), (18, 386, 1), (18, 514, 1), (18, 6369, 4467),
+         (18, 6592, 8446), (18, 6688, 4367), (19, 384, 1), (19, 393, 1), (19, 448, 1), (19, 6918, 4587),
+         (19, 7424, 4757), (25, 321, 1), (33, 129, 8422), (34, 6339, 4540), (35, 130, 5545), (37, 67, 8684),
+         (37, 128, 8879), (50, 64, 8341), (66, 139, 6083), (66, 3776, 5273), (66, 4274, 4180), (66, 4516, 8705),
+         (66, 5763, 6497), (66, 6627, 2942), (70, 6714, 5486), (71, 170, 8523), (71, 4672, 4116), (72, 3456, 8925),
+         (75, 3713, 4254), (113, 1, 8726), (130, 67, 6825), (131, 133, 7003), (138, 128, 6894), (203, 73, 4851),
+         (222, 130, 8490), (225, 137, 4116), (228, 72, 8769), (240, 64, 8905), (301, 68, 6606), (322, 1, 6917),
+         (322, 151, 5743), (452, 192, 4307), (491, 128, 4111), (518, 64, 8447), (584, 72, 1681), (585, 6592, 579),
+         (693, 2624, 1), (711, 3520, 1), (721, 2564, 1), (723, 3648, 1), (747, 3110, 1), (769, 3053, 1),
+         (771, 2887, 1), (813, 2564, 1), (828, 2624, 1), (850, 8, 5277), (933, 1, 8843), (988, 64, 8362),
+         (1061, 2358, 1), (1132, 8, 918), (1180, 1756, 1), (1238, 1922, 1), (1349, 129, 705), (1368, 1, 6716),
+         (1384, 7123, 1), (1887, 64, 8770), (1949, 9, 4141), (1957, 192, 531), (1964, 8, 1052), (2013, 8, 8954),
+         (2019, 1, 8758), (2059, 4800, 1), (2101, 6144, 1), (2145, 4480, 1), (2415, 4166, 1), (2710, 1, 1705),
+         (2721, 1, 707), (2749, 3264, 1), (2764, 2754, 1), (2803, 3460, 1), (2825, 2721, 1), (2967, 8, 3285),
+         (3089, 3617, 1), (3146, 64, 1299), (3225, 2900, 1), (3266, 8, 267), (3295, 64, 291), (3383, 128, 265),
+         (3431, 3015, 1), (3469, 1, 1154), (3557, 1, 257), (3781, 64, 2437), (4100, 64, 1), (4107, 1, 1),
+         (4113, 64, 1), (4113, 64, 33), (4120, 150, 36), (4124, 8, 559), (4127, 64, 203), (4147, 80, 37),
+         (4158, 192, 41), (4170, 69, 34), (4231, 1, 101), (4283, 9, 67), (4314, 8, 1), (4320, 1, 35),
+         (4325, 8512, 66), (4327, 1, 1), (4340, 192, 217), (4366, 128, 66), (4433, 8, 106), (4451, 1, 68),
+         (4467, 6021, 74), (4472, 192, 82), (4476, 8321, 66), (4489, 8643, 41), (4503, 8, 1), (4504, 128, 33),
+         (4542, 8, 39), (4547, 64, 66), (4676, 71, 195), (4771, 67, 68), (4787, 8, 844), (4847, 5379, 77),
+         (4872, 64, 387), (4965, 135, 66), (4978, 142, 69), (4983, 73, 69)]
 SHAPES += LARGE + TILES
 
 
