@@ -699,8 +699,8 @@ typedef struct vt_linear_io {
 vt_status vt_linear_workspace_size(const vt_linear_io* io, size_t* bytes);
 
 /* y = act(x w^T + bias) + residual, in one launch. A row's result does not depend on the rows
- * beside it but for the order of its fp32 sums, which n_rows, n_in and n_out decide; equal calls give equal
- * bits. Products of 2^22 tiles or more (of 256 rows x 256 features where there are many of both) are refused. */
+ * beside it but for the order of its fp32 sums, which the sizes, the places of the row and of the feature and the matrices' strides
+ * and alignment decide; equal calls give equal bits. Products of 2^22 tiles or more (of 256 rows x 256 features where there are many of both) are refused. */
 vt_status vt_linear(const vt_linear_io* io, void* ws, size_t ws_bytes, void* stream);
 
 /* y = act(x w^T + bias) * (x w_up^T + bias_up) + residual: both projections of a gated feed-forward
