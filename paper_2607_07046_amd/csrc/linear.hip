@@ -59,9 +59,10 @@ constexpr Cost kWideCost = {3.319, 0.8613, 9.745, 0.0473, 0.0299, 0, 0, 0};
 constexpr int kSlices[] = {1, 2, 3, 4, 6, 8, 12, 16};
 constexpr int kThinRows = 16;  // beyond, the thin tile reads the weights more than once
 constexpr int kUnits = 256;    // compute units
-// Where rows do not start at 128-byte lines, the tiles of 64 rows and more of linear_mid.hip load whole lines: 10 to 30% faster
-// with the weights in memory, 6% slower to 5% faster with weights still in the caches, 30% faster from 64 MB on. The smaller
-// tiles do for weights of this size (4 to 10% faster; below, no gain, and 15% slower in the caches).
+// Where rows do not start at 128-byte lines, the tiles of 64 rows and more of linear_mid.hip load whole lines: 10 to
+// 30% faster with the weights in memory, 6% slower to 5% faster with weights still in the caches, 30% faster from 64
+// MB on. The smaller tiles do for weights of this size (4 to 10% faster; below, no gain, and 15% slower in the
+// caches).
 constexpr int64_t kLinesFrom = int64_t(32) << 20;
 
 enum Kernel { kUseThin, kUseMid, kUseTile };

@@ -53,10 +53,11 @@ __device__ __forceinline__ bool my_tile(int id, int m_tiles, int cols, int tile_
   return true;
 }
 
-// Where an XCD starts in the n (>= 1) k-tiles of its slice; it goes on to the end and then from the beginning. Row strides are
-// multiples of large powers of two as a rule, and the same columns of all rows lie in few of memory's channels: were all
-// workgroups at the same columns, they would wait for those. One row of 8192 through 8192 features 35 -> 28 us,
-// 64 through the gate and up projections of 7168 65 -> 50 (weights in memory); products of more than 512 rows up to 5%.
+// Where an XCD starts in the n (>= 1) k-tiles of its slice; it goes on to the end and then from the beginning. Row
+// strides are multiples of large powers of two as a rule, and the same columns of all rows lie in few of memory's
+// channels: were all workgroups at the same columns, they would wait for those. One row of 8192 through 8192 features
+// 35 -> 28 us, 64 through the gate and up projections of 7168 65 -> 50 (weights in memory); products of more than 512
+// rows up to 5%.
 __device__ __forceinline__ int first_of(int id, int n) { return id % kXcds * n / kXcds; }
 
 // The activation functions in fp32. Half a step of the results' type is 2^-12 at least; exp2 and
@@ -122,8 +123,8 @@ __device__ __forceinline__ float one(const uint16_t* p) {
   return a;
 }
 
-// The first numbers of a group of W (4 or 8), fewer than W and as many in every lane: in pieces of 4, 2 and 1, whose places
-// are the same for all lanes.
+// The first numbers of a group of W (4 or 8), fewer than W and as many in every lane: in pieces of 4, 2 and 1, whose
+// places are the same for all lanes.
 template <int W, class V>
 __device__ __forceinline__ void store_first(uint16_t* y, V v, int count) {
   int at = 0;
@@ -142,10 +143,10 @@ __device__ __forceinline__ void store_first(uint16_t* y, V v, int count) {
   if (count & 1) y[at] = static_cast<uint16_t>(lo);
 }
 
-// W (4 or 8) consecutive features n.. of row m, from the product's sums to y. Whole groups by wide
-// accesses; of the group that reaches past N the bias is read by single numbers, the residual as it is (rows may be read up to a
-// multiple of 8) and nothing past N is written. (Both paths end in the same vector:
-// stores to z and u on either side of the branch were merged into one at a variable index, in scratch memory.)
+// W (4 or 8) consecutive features n.. of row m, from the product's sums to y. Whole groups by wide accesses; of the
+// group that reaches past N the bias is read by single numbers, the residual as it is (rows may be read up to a
+// multiple of 8) and nothing past N is written. (Both paths end in the same vector: stores to z and u on either side
+// of the branch were merged into one at a variable index, in scratch memory.)
 template <class T, bool GATED, int W>
 __device__ __forceinline__ void finish(const Args& a, int m, int n, float (&z)[W], float (&u)[W]) {
   typedef unsigned int vec __attribute__((ext_vector_type(W / 2)));

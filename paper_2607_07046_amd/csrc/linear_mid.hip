@@ -5,11 +5,12 @@
 // ring of ST stages of 64 k, up to ST - 1 of them on the way, each number once per tile; the
 // waves wait for a stage by the count of their own loads and meet once per stage.
 //
-// On tiles of 32 rows and more two waves share a place and take one of a stage's two k-steps each (KW = 2): a place can
-// then be twice as high, and LDS, which bounds these tiles, is read two thirds as much (128 x 128: 64 KiB of a stage, not 96). The
-// next stage's fragments are read, and loads sent out, between single products. The two waves' sums meet in LDS at the end, half
-// of the rows for each. A stage takes 0.098 us at 32 x 64, 0.125 at 64 x 64, 0.175 at 64 x 128 and 0.278 at 128 x 128, where one wave per
-// place that read, then multiplied took 0.148, 0.190, 0.259 and 0.414.
+// On tiles of 32 rows and more two waves share a place and take one of a stage's two k-steps each (KW = 2): a place
+// can then be twice as high, and LDS, which bounds these tiles, is read two thirds as much (128 x 128: 64 KiB of a
+// stage, not 96). The next stage's fragments are read, and loads sent out, between single products. The two waves'
+// sums meet in LDS at the end, half of the rows for each. A stage takes 0.098 us at 32 x 64, 0.125 at 64 x 64, 0.175
+// at 64 x 128 and 0.278 at 128 x 128, where one wave per place that read, then multiplied took 0.148, 0.190, 0.259
+// and 0.414.
 //
 // The product's first operand is the weights: a lane's accumulators are consecutive features of a row. The weight
 // rows of two blocks are dealt to them four by four in turn, so a lane has 8 consecutive features,
@@ -20,22 +21,23 @@
 // Rows past the matrices' ends are read from their last row (the sums are never stored). The stage that reaches
 // past K goes through registers, masked, and is multiplied first.
 //
-// Where rows do not start at 128-byte lines, 128 bytes of a row are in two lines, and each line is asked for twice, half of it
-// a time, which memory serves at half its rate. SHIFT loads whole lines: a stage holds a line of each row, from the one of
-// the row's start on, whose last chunks are the row's next ones. They lie where a row's chunks always do, so reads meet no
-// bank conflict, and a lane takes its chunk from a stage or from the next one. Since 8 rows are whole lines, which of them depends on
-// the row within the fragment alone: a lane's place in LDS is its own, and goes round the ring. It
-// keeps one more stage; the stage past K comes last and its fragments are masked.
-// The matrices themselves have to start at lines, else there would be reads before them. (Measured, bf16: 64 rows of 4104 numbers
-// through 14336 features 39 -> 28 us, as at 4096; with the weights in memory 640 rows of 3920 through 11678 118 -> 84; what the choice costs elsewhere is in linear.hip. With chunks where
-// they lie in their lines, conflicts in LDS cost half of that again.)
+// Where rows do not start at 128-byte lines, 128 bytes of a row are in two lines, and each line is asked for twice,
+// half of it a time, which memory serves at half its rate. SHIFT loads whole lines: a stage holds a line of each row,
+// from the one of the row's start on, whose last chunks are the row's next ones. They lie where a row's chunks always
+// do, so reads meet no bank conflict, and a lane takes its chunk from a stage or from the next one. Since 8 rows are
+// whole lines, which of them depends on the row within the fragment alone: a lane's place in LDS is its own, and goes
+// round the ring. It keeps one more stage and K's order; the stage past K comes last, its fragments masked. The matrices
+// themselves have to start at lines, else there would be reads before them. (Measured, bf16: 64 rows of 4104 numbers
+// through 14336 features 39 -> 28 us, as at 4096; with the weights in memory 640 rows of 3920 through 11678 118 ->
+// 84; what the choice costs elsewhere is in linear.hip. With chunks where they lie in their lines, conflicts in LDS
+// cost half of that again.)
 //
-// What bounds it: up to about 64 rows reading the weights, above it LDS (at 128 x 128 the products of a stage take 512 cycles, the
-// fragments' reads 512 and the loads' writes 256; it takes about 650). Measured in bf16: 64 rows of 8192 through the gate and
-// up projections of 7168 features 48 to 55 us, 4.3 to 4.9 TB/s; rows of 4096 through 4096 features: 256 rows 16 us
-// (530 TFLOP/s), 512 23 (760), 1024 34 (1010); 777 rows of 3302 through 4096 with a residual 32. Tried at 128 x 128 and not
-// kept: a quarter of the products ahead of the meeting point, no faster; the large tile's schedule for four waves; three stages of 64 x 128,
-// so that two workgroups fit, 1% slower.
+// What bounds it: up to about 64 rows reading the weights, above it LDS (at 128 x 128 the products of a stage take
+// 512 cycles, the fragments' reads 512 and the loads' writes 256; it takes about 650). Measured in bf16: 64 rows of
+// 8192 through the gate and up projections of 7168 features 48 to 55 us, 4.3 to 4.9 TB/s; rows of 4096 through 4096
+// features: 256 rows 16 us (530 TFLOP/s), 512 23 (760), 1024 34 (1010); 777 rows of 3302 through 4096 with a residual
+// 32. Tried at 128 x 128 and not kept: a quarter of the products ahead of the meeting point, no faster; the large
+// tile's schedule for four waves; three stages of 64 x 128, so that two workgroups fit, 1% slower.
 #include "linear_lds.hpp"
 
 namespace vt {
@@ -133,8 +135,8 @@ __global__ void __launch_bounds__(WR* WC* KW* kWave) mid_kernel(Args a) {
     constexpr int q = decltype(Q)::value;
     if (q > 0 || !tail || SHIFT) load(q * STAGE);
   });
-  // Where this lane's parts of the fragments are (in the block of their first row, with SHIFT in the ring): of rows, and of the
-  // gate's and the up projection's even and odd blocks, for both k-steps.
+  // Where this lane's parts of the fragments are (in the block of their first row, with SHIFT in the ring): of rows,
+  // and of the gate's and the up projection's even and odd blocks, for both k-steps.
   uint32_t fx[HS], fw[GATED ? 2 : 1][2][HS];
   auto spot = [&](int row, int64_t ld, int h) {
     const int ks = kw * HS + h, chunk = 4 * ks + lane / 16;
@@ -204,8 +206,8 @@ __global__ void __launch_bounds__(WR* WC* KW* kWave) mid_kernel(Args a) {
     constexpr int P = MBW * NBW;
     static_assert(MBW + NBW <= P && LPS <= P, "room beside the products");
     constexpr bool ROOM = 2 * LPS <= P;
-    // A stage is one k-step of this wave. The next one's fragments are read beside its products, so its own are in registers when
-    // the waves meet, and the stage is free for the loads.
+    // A stage is one k-step of this wave. The next one's fragments are read beside its products, so its own are in
+    // registers when the waves meet, and the stage is free for the loads.
     meet(std::integral_constant<int, SHIFT ? ST - 2 : ST - 1>{});
     read(S0{}, 0, 0);
     auto step = [&](auto SET) {

@@ -8,9 +8,9 @@
 // only stand in between. The waves' sums meet in LDS, in wave order; slices of K over several workgroups meet
 // in the workspace, added in slice order by whichever arrives last, which waits for nobody.
 //
-// What bounds it: reading the weights, and for small ones the chain launch -> loads -> join. Measured in captured graphs: one
-// row of 512 through 1536 features 3.7 to 4.3 us; one row of 4096 through the gate and up projections of 3302 features (54 MB)
-// 12.0 to 12.6 us, 4.3 to 4.5 TB/s, where a copy of 4 GiB reaches 4.7.
+// What bounds it: reading the weights, and for small ones the chain launch -> loads -> join. Measured in captured
+// graphs: one row of 512 through 1536 features 3.7 to 4.3 us; one row of 4096 through the gate and up projections of
+// 3302 features (54 MB) 11.7 to 12.4 us, 4.4 to 4.6 TB/s, where a copy of 4 GiB reaches 4.7.
 #include "linear.hpp"
 
 namespace vt {

@@ -1,11 +1,11 @@
 // Products of many rows: vt_linear and vt_linear_gated on tiles of 256 rows x 256 or 128 weight rows.
 //
-// Four waves, one per SIMD, of 128 x 128 each (accumulators in all 256 AGPRs) or 128 x 64. Both operands go from memory
-// straight into LDS, 16 bytes a lane and 1 KiB an instruction, in k-tiles of 64 through a ring of five half-tiles;
-// a wave multiplies one k-step of 32 while it reads the next one's fragments and sends its share of the loads of a
-// k-tile further on, so that nothing stands between two products for longer than the first of them takes. A gated
-// product's weight blocks are half a wave's of the gate and half of the up projection in turn, for the same features, so a
-// feature's two sums are in the same lane.
+// Four waves, one per SIMD, of 128 x 128 each (accumulators in all 256 AGPRs) or 128 x 64. Both operands go from
+// memory straight into LDS, 16 bytes a lane and 1 KiB an instruction, in k-tiles of 64 through a ring of five
+// half-tiles; a wave multiplies one k-step of 32 while it reads the next one's fragments and sends its share of the
+// loads of a k-tile further on, so that nothing stands between two products for longer than the first of them takes.
+// A gated product's weight blocks are half a wave's of the gate and half of the up projection in turn, for the same
+// features, so a feature's two sums are in the same lane.
 //
 // The product's first operand is the weights: a lane's four accumulators are then four consecutive features of a
 // row, one 16-byte store each on the way through LDS to the epilogue, in which 16 lanes take a row's
@@ -14,10 +14,10 @@
 // Rows past the matrices' ends are read from their last row (the sums are never stored). A last k-tile that
 // reaches past K goes through registers, masked, and is multiplied first.
 //
-// What bounds it: the matrix units, 1450 TFLOP/s at 8192 x 8192 x 8192 in bf16 (757 us); then the rounds of compute units that do not
-// come out even, and the epilogue, which nothing overlaps. 4096 rows of 5120 through 13824 features with bias and GELU in
-// fp16 480 to 505 us, 460 without the activation; of 4096 through a gate and an up projection of 11008
-// features each 535 to 558 us in bf16, 1320 to 1380 TFLOP/s.
+// What bounds it: the matrix units, 1450 TFLOP/s at 8192 x 8192 x 8192 in bf16 (757 us); then the rounds of compute
+// units that do not come out even, and the epilogue, which nothing overlaps. 4096 rows of 5120 through 13824 features
+// with bias and GELU in fp16 480 to 505 us, 460 without the activation; of 4096 through a gate and an up projection
+// of 11008 features each 535 to 558 us in bf16, 1320 to 1380 TFLOP/s.
 #include "linear_lds.hpp"
 
 namespace vt {

@@ -52,9 +52,10 @@ __device__ __forceinline__ S row_sum(S v, S* red) {
   return s;
 }
 
-// h = x + partial + peer, y = h / sqrt(mean(h^2) + eps) * gain. TR threads take a row and hold it in registers,
-// V groups of 8 numbers each, so every number is read and written once: memory bounds it. Measured: 8192 rows of 5120 with a
-// partial sum, bf16, 67 to 69 us, 4.9 to 5.0 TB/s; 64 rows of 8192 with a partial and the peers' sum 4.3 us in a captured graph.
+// h = x + partial + peer, y = h / sqrt(mean(h^2) + eps) * gain. TR threads take a row and hold it in registers, V
+// groups of 8 numbers each, so every number is read and written once: memory bounds it. Measured: 8192 rows of 5120
+// with a partial sum, bf16, 67 to 69 us, 4.9 to 5.0 TB/s; 64 rows of 8192 with a partial and the peers' sum 4.3 us in
+// a captured graph.
 constexpr int threads(int tr) { return tr <= 128 ? 256 : tr; }
 
 template <class T, int TR, int V>
@@ -161,8 +162,8 @@ namespace {
 
 constexpr int kMaxRows = 1 << 20, kMaxHidden = 16384;
 
-// The fewest threads, in whole waves, that hold a row: idle ones cost (8192 rows of 2049 numbers on 512 threads 39 us, on 320 35; of 5120
-// on 1024 71, on 640 69).
+// The fewest threads, in whole waves, that hold a row: idle ones cost (8192 rows of 2049 numbers on 512 threads 39
+// us, on 320 35; of 5120 on 1024 71, on 640 69).
 template <class T, int V, int TR, int... MORE>
 void launch_norm(const rows::NormArgs& a, hipStream_t s) {
   if constexpr (sizeof...(MORE) > 0)
