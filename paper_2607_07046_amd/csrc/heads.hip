@@ -28,13 +28,13 @@ struct HeadsArgs {
 
 // Eight numbers as e4m3: number / scale, rounded to nearest even, saturating; NaN stays. The quotient is the product
 // with the reciprocal and one correction, which leaves a division's result (an exact quotient that lies between
-// two e4m3 numbers must not move).
+// two e4m3 numbers must not move) but for the sign of a zero: the remainder of -0 is +0, and so would be its quotient.
 __device__ __forceinline__ u32x2 scaled_to_f8(const float (&x)[8], float scale, float rcp) {
   float y[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
     const float q = x[e] * rcp, d = fmaf(fmaf(-q, scale, x[e]), rcp, q);
-    y[e] = fabsf(q) > kF8Max ? copysignf(kF8Max, q) : d;
+    y[e] = copysignf(fabsf(q) > kF8Max ? kF8Max : d, q);
   }
   u32x2 r;
 #pragma unroll
