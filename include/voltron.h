@@ -745,7 +745,7 @@ typedef struct vt_rope {
   float low;
   float high;              /* above low, or both 0 */
   int32_t context;         /* >= 1 with low or high */
-  float amplitude;         /* > 0; 0 stands for 1 */
+  float amplitude;         /* > 0; 0 stands for 1. Its products with a head norm's gains are taken in fp32 */
 } vt_rope;
 
 /* Norms per head, before the rotation: x / sqrt(mean(x^2) + eps) * gain over the head's numbers. */

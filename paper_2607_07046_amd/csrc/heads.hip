@@ -46,7 +46,7 @@ __device__ __forceinline__ u32x2 scaled_to_f8(const float (&x)[8], float scale, 
 }
 
 // A workgroup takes one row, or for few rows a part of its heads; a wave's turn is 512 numbers of them, 8 per lane.
-//   y_i = (x_i g_i) cos_i +- (x_j g_j) sin_i = inv (x_i A_i + x_j B_i),  j the number that i turns with:
+//   y_i = (inv x_i) g_i cos_i +- (inv x_j) g_j sin_i = (inv x_i) A_i + (inv x_j) B_i,  j the number that i turns with:
 // A and B are the same for all of a row's query heads and for all of its key heads and are made once, in LDS.
 // With HALVES x_j is in another lane: the head's 16-bit numbers go through LDS, in one 16-byte read where the
 // halves are multiples of 8. Keys, values and queries start at whole turns of a wave, so what is done is the
@@ -161,15 +161,23 @@ __global__ void __launch_bounds__(HT, 6) heads_kernel(HeadsArgs a, Freq f) {
     float x[8];
     unpack(w, x);
     if (kind != V) {
-      float inv = 1.f, o[8];
+      float o[8];
       partners(w, o);
       if (kind == Q ? a.q_gain != nullptr : a.k_gain != nullptr) {
         float ss = 0.f;
 #pragma unroll
         for (int e = 0; e < 8; ++e) ss = fmaf(x[e], x[e], ss);
         const float mean = group_sum(ss, CPR) * (1.f / D) + a.eps;
-        inv = __builtin_amdgcn_rsqf(mean);
-        if (!(mean > 1e-30f && mean < 1e37f)) {
+        // Numbers are normalised before they meet A and B: the product of a large one with a large gain, or of two small
+        // ones, would leave fp32's range where the result does not.
+        if (mean > 1e-30f && mean < 1e37f) {
+          const float inv = __builtin_amdgcn_rsqf(mean);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            x[e] *= inv;
+            o[e] *= inv;
+          }
+        } else {
           // Squares of bf16 numbers leave fp32's range at 2^64 and 2^-63: such a head's statistics and its first
           // products are taken in double.
           double s2 = 0.0;
@@ -183,7 +191,6 @@ __global__ void __launch_bounds__(HT, 6) heads_kernel(HeadsArgs a, Freq f) {
             x[e] = static_cast<float>(x[e] * wide);
             o[e] = static_cast<float>(o[e] * wide);
           }
-          inv = 1.f;
         }
       }
       const f32x4* ab = reinterpret_cast<const f32x4*>(coef[kind == Q] + c * CS);
@@ -194,7 +201,7 @@ __global__ void __launch_bounds__(HT, 6) heads_kernel(HeadsArgs a, Freq f) {
         for (int q = 0; q < 4; ++q) {
           const int e = 4 * v + q;
           const float own = x[e] * ca[q], both = fmaf(o[e], cb[q], own);
-          x[e] = inv * (all || e < turned ? both : own);  // (infinity times a zero B would be NaN)
+          x[e] = all || e < turned ? both : own;  // (infinity times a zero B would be NaN)
         }
       }
 #pragma unroll

@@ -7,6 +7,7 @@ import torch
 from paper_2607_07046_amd import voltron as vt
 from tests.paged_common import F8, Batch
 from tests.rows_common import p, stream
+from tests.test_gpu_rows import Heads, check_append, gains_of
 
 pytestmark = pytest.mark.gpu
 BOTH = pytest.mark.parametrize("type", ["f16", "bf16"])
@@ -70,3 +71,56 @@ def test_bytes_of_a_plain_append(type, f8, scales):
         stored.append(pools(b))
     for one, other in zip(*stored):
         assert torch.equal(one, other)
+
+
+# Sizes of the numbers and of the gains: products of a number with its gain beyond the range of fp32 although the
+# normalised number's are far inside it; products that have no full precision in fp32; numbers past both borders of the
+# fast statistics.
+FAR = pytest.mark.parametrize("size,gain,eps", [(1e18, 1e21, 1e-5), (1e-14, 1e-30, 0.0), (1e-14, 1e30, 0.0),
+                                                (1e18, 1e-30, 1e-5), (1.0, 1e37, 1e-6), (1.0, 1e-36, 1e-6), (1e25, 1e25, 1e-5),
+                                                (1e-30, 1e-12, 0.0)])
+TURNS = pytest.mark.parametrize("rope", [None, dict(base=10000.0), dict(base=10000.0, flags=1),
+                                         dict(base=500000.0, dims=50, flags=1, amplitude=0.75)])
+
+
+def scaled(t, by):
+    """Numbers of |x| up to 1 times ``by``."""
+    t.copy_((t.double().clamp(-1, 1) * by).to(t.dtype))
+
+
+@FAR
+@TURNS
+@pytest.mark.parametrize("d", [64, 128])
+def test_head_norms_with_far_gains(size, gain, eps, rope, d):
+    """Whatever the sizes of numbers and gains, results that bf16 holds are right. Tolerances as everywhere; numbers
+    below fp32's normal ones (2^-126) may count as zero."""
+    x = Heads("bf16", 7, 5, 3, d, eps=eps, far=300)
+    for t in (x.q, x.k):
+        scaled(t, size)
+    for t in (x.q_gain, x.k_gain):
+        scaled(t, gain)
+    x.call(rope)
+    ref = {n: x.reference(n, rope, x.pos) for n in ("q", "k")}
+    assert all(float(w.abs().max()) < 3e38 for w, _ in ref.values())
+    x.check(rope, ref={n: (w, t + 2.0 ** -126) for n, (w, t) in ref.items()})
+
+
+@pytest.mark.parametrize("size,gain,eps", [(1e18, 1e21, 1e-5), (1e-14, 1e30, 0.0)])
+@pytest.mark.parametrize("flags", [0, 1])
+def test_append_with_far_gains(size, gain, eps, flags):
+    b = Batch([40, 17], [7, 17], kv_heads=3, group=2, d=128, act="bf16")
+    gains = gains_of(b)
+    for t in gains:
+        scaled(t, gain)
+    before = {n: b.slots(getattr(b, n + "_pool")).clone() for n in ("k", "v")}
+    g = torch.Generator(device="cuda").manual_seed(1)
+    qkv = torch.empty((b.n_tok, (b.nq + 6) * 128), dtype=b.dtype, device="cuda").normal_(generator=g)
+    scaled(qkv, size)
+    q, k, v = qkv[:, :b.nq * 128], qkv[:, b.nq * 128:-3 * 128], qkv[:, -3 * 128:]
+    q_rot = torch.empty((b.n_tok, b.nq * 128), dtype=b.dtype, device="cuda")
+    rope = dict(base=10000.0, flags=flags)
+    io = b.io(q=p(q), ld_q=qkv.stride(0), k=p(k), ld_k=qkv.stride(0), v=p(v), ld_v=qkv.stride(0), q_rot=p(q_rot))
+    vt.vt_paged_append_heads(b.kv(), io, vt.vt_head_norm(q_gain=p(gains[0]), k_gain=p(gains[1]), eps=eps), vt.vt_rope(**rope),
+                             stream())
+    torch.cuda.synchronize()
+    check_append(b, rope, gains, eps, q, k, v, q_rot, before)
