@@ -71,6 +71,7 @@ struct Plan {
   Kernel kernel;
   int mid;     // of kMid
   int m_tiles, n_tiles, wide, splits, steps;
+  bool lines;  // kUseMid: whole lines of rows that do not start at them
   double us;
 };
 
@@ -109,7 +110,7 @@ Plan plan_of(int64_t M, int64_t N, int64_t K, bool gated) {
       const double us = c.start + rounds * (c.step * steps + c.tile) + c.memory * mb + c.l2 * loads +
                         (splits > 1 ? c.join + c.part * 1e-6 * part + c.slice * splits : 0.0);
       if (us < best.us)
-        best = {kernel,  mid, static_cast<int>(mt), static_cast<int>(nt), 0, static_cast<int>(splits), static_cast<int>(steps), us};
+        best = {kernel,  mid, static_cast<int>(mt), static_cast<int>(nt), 0, static_cast<int>(splits), static_cast<int>(steps), false, us};
     }
   };
   if (M <= kThinRows) consider(kUseThin, 0, lin::kThin, kThinCost);
@@ -129,7 +130,7 @@ Plan plan_of(int64_t M, int64_t N, int64_t K, bool gated) {
                                           kNarrowCost.step * all + kNarrowCost.tile) +
                         c.memory * mb + c.l2 * loads;
       if (us < best.us)
-        best = {kUseTile, 0, static_cast<int>(mt), static_cast<int>(n), static_cast<int>(w), 1, static_cast<int>(all), us};
+        best = {kUseTile, 0, static_cast<int>(mt), static_cast<int>(n), static_cast<int>(w), 1, static_cast<int>(all), false, us};
     };
     tile(0);
     tile(cols);
@@ -140,6 +141,15 @@ Plan plan_of(int64_t M, int64_t N, int64_t K, bool gated) {
     }
   }
   return best;
+}
+
+Plan plan_of(const vt_linear_io& io, bool gated) {
+  Plan p = plan_of(io.n_rows, io.n_out, io.n_in, gated);
+  const auto line = [](const void* q) { return reinterpret_cast<uintptr_t>(q) % 128 == 0; };
+  p.lines = p.kernel == kUseMid && (io.ld_x | io.ld_w | (gated ? io.ld_up : 0)) % 64 != 0 && line(io.x) && line(io.w) &&
+            (!gated || line(io.w_up)) &&
+            (lin::kMid[p.mid].rows >= 64 || static_cast<int64_t>(io.n_in) * io.n_out * (gated ? 4 : 2) >= kLinesFrom);
+  return p;
 }
 
 vt_status project(const vt_linear_io* io, bool gated, void* ws, size_t ws_bytes, void* stream) {
@@ -181,7 +191,7 @@ vt_status project(const vt_linear_io* io, bool gated, void* ws, size_t ws_bytes,
   a.N = io->n_out;
   a.K = io->n_in;
   a.act = io->act;
-  const Plan p = plan_of(a.M, a.N, a.K, gated);
+  const Plan p = plan_of(*io, gated);
   a.m_tiles = p.m_tiles;
   a.n_tiles = p.n_tiles;
   a.wide = p.wide;
@@ -192,13 +202,9 @@ vt_status project(const vt_linear_io* io, bool gated, void* ws, size_t ws_bytes,
   if (lin::grid_of(p.m_tiles, static_cast<int64_t>(p.n_tiles) * p.splits) + lin::grid_of(p.m_tiles, p.wide) >= (int64_t(1) << 22))
     return fail(VT_ERR_UNSUPPORTED, "%d x %d tiles: fewer rows or features per call", p.m_tiles, p.n_tiles + p.wide);
   const bool bf16 = io->type == VT_T_BF16;
-  const auto line = [](const void* q) { return reinterpret_cast<uintptr_t>(q) % 128 == 0; };
-  const bool shift = (io->ld_x | io->ld_w | (gated ? io->ld_up : 0)) % 64 != 0 && line(a.x) && line(a.w[0]) &&
-                     (!gated || line(a.w[1])) &&
-                     (lin::kMid[p.mid].rows >= 64 || K * N * (gated ? 4 : 2) >= kLinesFrom);
   const hipStream_t s = static_cast<hipStream_t>(stream);
   const hipError_t e = p.kernel == kUseThin  ? lin::launch_thin(a, bf16, gated, s)
-                       : p.kernel == kUseMid ? lin::launch_mid(a, p.mid, shift, bf16, gated, s)
+                       : p.kernel == kUseMid ? lin::launch_mid(a, p.mid, p.lines, bf16, gated, s)
                                              : lin::launch_tile(a, bf16, gated, s);
   return e == hipSuccess ? VT_OK : fail(VT_ERR_HIP, "projection launch: %s", hipGetErrorString(e));
 }
@@ -222,4 +228,14 @@ extern "C" vt_status vt_linear(const vt_linear_io* io, void* ws, size_t ws_bytes
 extern "C" vt_status vt_linear_gated(const vt_linear_io* io, void* ws, size_t ws_bytes, void* stream) {
   clear_error();
   return project(io, true, ws, ws_bytes, stream);
+}
+
+// For the tests: what a product is given to. out: the kernel (0 thin, 1 .. 5 of kMid, 6 tile), slices of K, k-steps of
+// 64 of a slice, columns of 256-feature tiles, columns of the others, whole-line loads. Nothing is read through io's pointers.
+extern "C" int vt_test_linear_plan(const vt_linear_io* io, int32_t gated, int32_t* out) {
+  const Plan p = plan_of(*io, gated != 0);
+  const int32_t all[] = {p.kernel == kUseThin ? 0 : (p.kernel == kUseMid ? 1 + p.mid : 1 + static_cast<int>(std::size(lin::kMid))),
+                         p.splits, p.steps, p.wide, p.n_tiles, p.lines};
+  std::copy(std::begin(all), std::end(all), out);
+  return static_cast<int>(std::size(all));
 }
