@@ -660,14 +660,18 @@ vt_status vt_paged_chunk_attn(const vt_paged_kv* kv, const vt_paged_io* io, floa
  * Numbers are VT_T_F16 or VT_T_BF16, one type for all operands of a call; sums, norms and
  * angles are fp32 or more, and each result is rounded once. Matrices are [rows][ld]: a row's numbers
  * from its length up to the next multiple of 8 may be read (whatever they hold, they change nothing) and
- * are never written. Infinities and NaN in a row or a weight reach the results as in the formulas. Everything
- * but the descriptors is device memory of the current device, and ``stream`` is one of that device. Up to 2^20
- * rows a call. The projections are fastest where rows start at 128-byte lines (x, w and w_up at such addresses, their ld
- * multiples of 64). Other row strides cost little up to a thousand rows and up to a third of a product of more rows; matrices that do
- * not even start at a line cost a third where reading the weights of a batch is all of the time. */
+ * are never written. Of a projection's x, w and w_up anything between the first row's start and the end of the
+ * last row's last group of 8 may be read, also what lies between two rows: other columns of a wider
+ * matrix, which may change meanwhile. Infinities and NaN in a row or a weight reach the results as in the
+ * formulas, but for VT_ACT_RELU, which takes NaN to 0. Everything but the descriptors is device memory of the
+ * current device, and ``stream`` is one of that device. Up to 2^20 rows a call.
+ * The projections are fastest where rows start at 128-byte lines (x, w and w_up at such addresses, their ld
+ * multiples of 64). Other row strides cost little up to a thousand rows and up to a third of a product of
+ * more rows; matrices that do not even start at a line cost a third where reading the weights of a batch is
+ * all of the time. */
 
 /* Activation functions: z, max(z, 0), z / (1 + exp(-z)), z Phi(z) with the normal distribution's
- * Phi, and its approximation z (1 + tanh(sqrt(2 / pi) (z + 0.044715 z^3))) / 2. VT_ACT_RELU of NaN is 0. */
+ * Phi, and its approximation z (1 + tanh(sqrt(2 / pi) (z + 0.044715 z^3))) / 2. VT_ACT_RELU of NaN is 0 (z > 0 ? z : 0). */
 enum { VT_ACT_NONE = 0, VT_ACT_RELU = 1, VT_ACT_SILU = 2, VT_ACT_GELU = 3, VT_ACT_GELU_TANH = 4 };
 
 /* A projection of rows. */
