@@ -62,8 +62,12 @@ __device__ __forceinline__ int first_of(int id, int n) { return id % kXcds * n /
 
 // The activation functions in fp32. Half a step of the results' type is 2^-12 at least; exp2 and
 // the reciprocal are the hardware's, a few 2^-24 off.
+//
+// 1 / (1 + exp(-z)), from numbers 2^-12 times as large: the hardware's reciprocal of one above 2^126 is 0, and z times
+// the sigmoid is a number that bf16 holds down to z = -92. (The exponent of a z near 0 rounds 2^-21 off.)
 __device__ __forceinline__ float sigmoid(float z) {
-  return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-kLog2e * z));
+  constexpr float small = 0x1p-12f;
+  return small * __builtin_amdgcn_rcpf(small + __builtin_amdgcn_exp2f(fmaf(-kLog2e, z, -12.f)));
 }
 
 // z Phi(z) with Phi(z) = erfc(-z / sqrt 2) / 2. erfc(x) = exp(-x^2) t Q(t), t = 1 / (1 + 0.54 x): the
