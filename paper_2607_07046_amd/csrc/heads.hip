@@ -53,10 +53,10 @@ __device__ __forceinline__ u32x2 scaled_to_f8(const float (&x)[8], float scale, 
 // same for all of its lanes. Every number is read and written once; the next turns' loads are in flight
 // while one is computed.
 // What bounds it: memory for many rows, the chain row -> sequence -> length -> page -> store for few. Measured: ragged
-// prompts, 10310 rows of 96 heads of 128, bf16 into 8-bit, half of each head turning: 94 us for 422 MB, 4.5 TB/s
+// prompts, 10310 rows of 96 heads of 128, bf16 into 8-bit, half of each head turning: 91 to 94 us for 422 MB, 4.6 TB/s
 // (a wave per row 96 to 164, the slower the more of them were at work; with A, B and the angles in each
-// lane's registers 139); 4096 rows of 64 heads without a cache 29 us, 4.6 TB/s; 64 rows of 80 heads 4.0 us in a
-// captured graph, one row 2.9.
+// lane's registers 139); 4096 rows of 64 heads without a cache 30 us, 4.5 TB/s; 64 rows of 80 heads 3.6 to
+// 4.0 us, one row 2.5 to 3.0 (all in captured graphs).
 template <class T, bool PAGED, bool F8, bool HALVES, int D>
 __global__ void __launch_bounds__(HT, 6) heads_kernel(HeadsArgs a, Freq f) {
   constexpr int CPR = D / 8, HL = kWave / CPR, B = 2;  // lanes of a head, heads of a turn, turns in flight

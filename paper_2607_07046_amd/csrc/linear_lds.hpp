@@ -1,8 +1,8 @@
 // Loads from memory straight into LDS, and the layout that the projections' kernels give them there.
 //
 // LDS holds blocks of 8 rows x 64 k (1 KiB): one instruction of a wave, whose 8 lanes of a row read a whole
-// 128-byte line (with 16 rows x 32 k every line was fetched twice, a product of 8192 x 8192 x 8192 took 843 us and
-// not 760). Chunk c (16 bytes) of row r of a fragment of 16 rows is at unit 8 (r % 8) + (c ^ (r / 2)) of block
+// 128-byte line (with 16 rows x 32 k every line was fetched twice, a product of 8192 x 8192 x 8192 took 843 us, where
+// it takes 743 to 757). Chunk c (16 bytes) of row r of a fragment of 16 rows is at unit 8 (r % 8) + (c ^ (r / 2)) of block
 // r / 8: the 16 lanes that a fragment's read serves together (0-3, 12-15, 20-23, 24-27 and the like)
 // find it in different banks.
 #pragma once

@@ -34,9 +34,9 @@
 //
 // What bounds it: up to about 64 rows reading the weights, above it LDS (at 128 x 128 the products of a stage take
 // 512 cycles, the fragments' reads 512 and the loads' writes 256; it takes about 650). Measured in bf16: 64 rows of
-// 8192 through the gate and up projections of 7168 features 48 to 55 us, 4.3 to 4.9 TB/s; rows of 4096 through 4096
-// features: 256 rows 16 us (530 TFLOP/s), 512 23 (760), 1024 34 (1010); 777 rows of 3302 through 4096 with a residual
-// 32. Tried at 128 x 128 and not kept: a quarter of the products ahead of the meeting point, no faster; the large
+// 8192 through the gate and up projections of 7168 features 47 to 49 us, 4.8 to 5.0 TB/s; rows of 4096 through 4096
+// features: 256 rows 16 us (540 TFLOP/s), 512 22 (780), 1024 33 (1040); 777 rows of 3302 through 4096 with a residual
+// 28 to 32. Tried at 128 x 128 and not kept: a quarter of the products ahead of the meeting point, no faster; the large
 // tile's schedule for four waves; three stages of 64 x 128, so that two workgroups fit, 1% slower.
 #include "linear_lds.hpp"
 

@@ -14,10 +14,11 @@
 // Rows past the matrices' ends are read from their last row (the sums are never stored). A last k-tile that
 // reaches past K goes through registers, masked, and is multiplied first.
 //
-// What bounds it: the matrix units, 1450 TFLOP/s at 8192 x 8192 x 8192 in bf16 (757 us); then the rounds of compute
-// units that do not come out even, and the epilogue, which nothing overlaps. 4096 rows of 5120 through 13824 features
-// with bias and GELU in fp16 480 to 505 us, 460 without the activation; of 4096 through a gate and an up projection
-// of 11008 features each 535 to 558 us in bf16, 1320 to 1380 TFLOP/s.
+// What bounds it: the matrix units, 1450 to 1480 TFLOP/s at 8192 x 8192 x 8192 in bf16 (743 to 757 us); then the
+// rounds of compute units that do not come out even, and the epilogue, which nothing overlaps and which is most of the
+// time where K is short (4096 rows of 64 through 4096 features 17 us for 35 MB). 4096 rows of 5120 through 13824
+// features with bias and GELU in fp16 468 to 494 us, 460 without the activation; of 4096 through a gate and an up
+// projection of 11008 features each 524 to 540 us in bf16, 1370 to 1410 TFLOP/s.
 #include "linear_lds.hpp"
 
 namespace vt {
